@@ -213,11 +213,10 @@ def _own_grad(state):
 def _own_balance(state):
     import paper_2303_08999_b200 as sr
     case = state["case"]
-    flags = BALANCE_PER_FRAME if case["per_frame"] else 0
-    loss, counts, valid, share = sr.sr_select_balance(state["coef"], state["idx"], state["mask"], flags)
-    grad = sr.sr_select_balance_grad(state["coef"], counts, valid, case["s"], state["mask"], state["weight"],
-                                     flags=flags | (GRAD_ADD if case["add"] else 0), grad_coef=state["grad"])
-    return loss, counts, share, grad
+    loss, counts, share, slope = sr.sr_select_balance(state["coef"], state["idx"], state["mask"], BALANCE_PER_FRAME if case["per_frame"] else 0)
+    grad = sr.sr_select_balance_grad(state["coef"], slope, state["mask"], state["weight"], flags=GRAD_ADD if case["add"] else 0,
+                                     grad_coef=state["grad"])
+    return loss, counts, share, slope, grad
 
 
 def _own_adamw(state):
@@ -311,7 +310,7 @@ def _plain_balance(state):
     grad = state["weight"] * torch.sign(value) * (a - (a * p).sum(1, keepdim=True)) / total * on
     grad = torch.where(total > 0, grad, 0.0)
     state["grad"].copy_(state["grad"].float() + grad if case["add"] else grad)
-    return loss.float().view(1), counts.int(), share.float(), state["grad"]
+    return loss.float().view(1), counts.int(), share.float(), a.view(n, D), state["grad"]
 
 
 def _e4m3(x, scale):
@@ -413,6 +412,7 @@ def _exact_balance(state):
     on = torch.ones((n, H, W), dtype=torch.float64, device="cuda") if state["mask"] is None else state["mask"].double()
     counts = torch.stack([torch.bincount((idx[f].long() + 1)[(on[f] > 0).expand(s, H, W)], minlength=D + 1)[1:] for f in range(n)])
     valid = on.sum((1, 2))
+    slope = counts.double() / s / (n * valid.clamp(min=1) ** 2).view(n, 1) if case["per_frame"] else (counts.sum(0) / s / valid.sum().clamp(min=1) ** 2).expand(n, D)
     loss, shares, grads = 0.0, [], []
     for f in range(n):
         coef = state["coef"][f].double().requires_grad_()
@@ -429,7 +429,7 @@ def _exact_balance(state):
     grad = torch.stack(grads)
     if case["add"]:
         grad += state["grad"]
-    return loss.view(1), counts.int(), torch.stack(shares), grad
+    return loss.view(1), counts.int(), torch.stack(shares), D * slope, grad
 
 
 def _exact_adamw(state):
