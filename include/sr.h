@@ -65,6 +65,7 @@ typedef struct sr_dims {
 } sr_dims;
 
 enum { SR_F32 = 0, SR_F16 = 1 }; /* coefficient storage type */
+enum { SR_BF16 = 2 };            /* sr_adamw_step only: bfloat16 parameters or gradients */
 
 enum {
     SR_CLAMP01 = 1u,      /* clamp the output to [0,1] as the last step                                */
@@ -86,6 +87,10 @@ enum {
                                   regression of the luma frame (the fast kernels) and two small kernels, using
                                   `out` itself as scratch; with binary16 / 8-bit output it runs on the general
                                   fp32 kernel.                                                                  */
+};
+enum {
+    SR_GRAD_ADD = 128u,         /* sr_select_balance_grad: add to grad_coef instead of writing it           */
+    SR_BALANCE_PER_FRAME = 256u /* sr_select_balance: every frame balanced by itself, the losses averaged   */
 };
 
 enum {
@@ -163,9 +168,10 @@ int sr_dict_regress_selected(const float* lr, const void* coef_or_sel, int coef_
  * Dictionary selection search (Section III-A).  The paper keeps alpha * L of the L atoms: a selecting vector beta
  * enters the filter as F = Phi diag(beta) D (Eq. 5-6), beta is found by LASSO (Eq. 7) with lambda doubled and then
  * bisected until about alpha_t L atoms survive, the coefficient layer is re-fitted on the survivors by least squares
- * (Eq. 9: one re-weight gamma_l per kept atom), and alpha_t is lowered step by step (Algorithm 1).  Fine-tuning the
- * whole network is not part of this library; the re-fit of Eq. 9 is the paper's own fast substitute for it.  The
- * result (atom ids + re-weights) is what sr_dict_regress_selected takes with SR_IDX_GLOBAL.
+ * (Eq. 9: one re-weight gamma_l per kept atom), and alpha_t is lowered step by step (Algorithm 1).  The search itself
+ * fine-tunes nothing: the re-fit of Eq. 9 is the paper's own fast substitute for it; the calls of the training section
+ * below are what a fine-tuning step (the W-step of Algorithm 1) of the dictionary, the re-weights and the network takes.
+ * The result (atom ids + re-weights) is what sr_dict_regress_selected takes with SR_IDX_GLOBAL.
  *
  * sr_selection_gram: everything the search needs from the images.  With z_l[i,c] = coef[l][i] * (dict[l] . B_{i,c})
  * the response of atom l alone at HR pixel i, channel c, and `target` [n][c][H][W] fp32 the ground-truth HR image:
@@ -305,6 +311,111 @@ int sr_producer_fold(const float* wconv, const float* bias, const float* dict, c
                      int s, void* folded, size_t folded_bytes, const sr_dims* d, int cin, int kc, void* stream);
 int sr_producer_regress(const float* lr, const void* feat, const void* folded, size_t folded_bytes, float* out,
                         const sr_dims* d, int cin, int kc, uint32_t flags, void* stream);
+
+/*
+ * Training: the gradients of the regression, the balance loss of a per-pixel selection, and the optimiser's step.
+ * Algorithm 1's W-step (Section III-A, Eq. 8) and the training that precedes it fine-tune the network's weights and the
+ * dictionary under a selection; these calls are that step's operators on this library's side of the network.
+ *
+ * sr_dict_regress_dense_grad / sr_dict_regress_selected_grad: with grad_out[n][c][H][W] = dL/d out (fp32) and
+ *     G_j(i) = sum_c grad_out_c(i) * B_{i,c}[j]                      (B the patch of the up-sampled image)
+ * the gradients of sr_dict_regress_dense, out = sum_j (sum_l coef_l dict[l][j]) B[j], are
+ *     grad_coef_l(i) = sum_j dict[l][j] G_j(i)                       [n][D][H][W], coefficient dtype
+ *     grad_dict[l][j] = sum_i coef_l(i) G_j(i)                       [D][k*k] fp32, summed over all frames and pixels
+ * and of sr_dict_regress_selected:
+ *   flags = 0             grad_coef [n][D][H][W]: the sum above for the s atoms that idx lists at the pixel, zero for the others;
+ *                         grad_dict sums over the pixels that list the atom.  (The choice itself has no gradient.)
+ *   SR_COEF_COMPACT       grad_coef [n][s][H][W], by rank like the values.
+ *   SR_IDX_GLOBAL         grad_coef_{a_q} = gamma_q sum_j dict[a_q][j] G_j ([n][D][H][W] with zero planes for atoms outside the
+ *                         subset; with SR_COEF_COMPACT [n][s][H][W]); with A_q[j] = sum_i w_q(i) G_j(i), w_q the plane's
+ *                         coefficient: grad_dict[a_q] = gamma_q A_q (zero rows outside), grad_gamma[q] = sum_j dict[a_q][j] A_q[j].
+ * idx is required (choose with sr_dict_select first).  grad_coef or grad_dict may be NULL: that gradient is then not computed, and with
+ * grad_dict NULL coef may be NULL; grad_gamma (SR_IDX_GLOBAL only) may be NULL and needs coef and gamma-weighted atoms as grad_dict does.
+ * Every element of the outputs asked for is written (nothing is added to).  flags: SR_UPSAMPLE_BILINEAR, and for the selected call
+ * SR_IDX_GLOBAL, SR_COEF_COMPACT.  SR_CLAMP01 is not a flag here: zero grad_out where the forward pass clamped.
+ * Distinct indices per pixel, and indices >= D, as in sr_dict_regress_selected (a repeated index of a pixel gives an unspecified
+ * gradient for it; with SR_IDX_GLOBAL repeated atoms are summed).  The outputs must not overlap each other or an input.
+ * Sums are held in fp32 or more; the same inputs give the same bits on every run.  A value of grad_out, of the image's patch or a
+ * coefficient that is not finite makes grad_coef of the pixels that read it and the grad_dict rows it enters not finite (Inf or NaN is
+ * unspecified); other pixels are as without it.  Gradients in binary16 are rounded once: scale a small loss up (loss scaling) first.
+ * `scratch`: device memory of sr_dict_regress_grad_scratch_bytes(d) bytes (for the current device), 16-byte aligned, needed
+ * when grad_dict or grad_gamma is asked for; the call overwrites it, and two calls that share it must not overlap.
+ */
+size_t sr_dict_regress_grad_scratch_bytes(const sr_dims* d);
+int sr_dict_regress_dense_grad(const float* lr, const void* coef, int coef_dtype, const float* dict, const float* grad_out,
+                               void* grad_coef, float* grad_dict, const sr_dims* d, uint32_t flags, void* scratch,
+                               size_t scratch_bytes, void* stream);
+int sr_dict_regress_selected_grad(const float* lr, const void* coef_or_sel, int coef_dtype, const uint8_t* idx, const float* gamma,
+                                  const float* dict, const float* grad_out, void* grad_coef_or_sel, float* grad_dict,
+                                  float* grad_gamma, const sr_dims* d, int s, uint32_t flags, void* scratch, size_t scratch_bytes,
+                                  void* stream);
+
+/*
+ * sr_select_balance: how evenly a per-pixel selection uses the atoms, as a loss.  With share p_l(i) = |coef_l(i)| / sum_m |coef_m(i)|
+ * (1/D each where the sum is below the smallest normal fp32 number), over the T valid pixels:
+ *     f_l = counts_l / (s T)   how often idx lists atom l,     P_l = sum_i p_l(i) / T,     loss = D sum_l f_l P_l
+ * (1 when atoms are used evenly).  With SR_BALANCE_PER_FRAME the loss is the mean over the n frames of the same expression
+ * per frame, otherwise the batch counts as one.  A frame (batch) without valid pixels contributes 0.
+ *   coef   [n][D][H][W], coef_dtype;  idx [n][s][H][W] as sr_dict_select writes it (an entry >= D is not counted)
+ *   mask   [n][H][W] uint8, 0 = the pixel does not count (padding): neither its coefficients, whatever they are, nor its
+ *          indices are used; NULL = every pixel counts
+ *   counts [n][D] int32, share [n][D] fp32 (each frame's mean p_l over its own valid pixels), loss [1] fp32
+ *   slope  [n][D] fp32: dL/dp_l of a valid pixel of the frame, what sr_select_balance_grad takes
+ * Counts are exact; sums are held in fp32 per block and fp64 across blocks; the same inputs give the same bits.
+ *
+ * sr_select_balance_grad: grad_coef_l(i) = weight * (*grad_loss) * sign(coef_l) / sum_m |coef_m| * (slope_l - sum_m slope_m p_m(i)),
+ * zero for pixels that do not count or whose sum is below the smallest normal number; counts have no gradient.  grad_loss: device
+ * fp32 [1] or NULL (1).  SR_GRAD_ADD adds it to grad_coef (read and rounded in the coefficient dtype; a pixel that does not count keeps
+ * its bits), e.g. to what the regression's gradient wrote.  The values are of the order weight / T: with binary16 use a loss scale.
+ * A valid pixel with a coefficient that is not finite, or whose sum overflows fp32, has an unspecified gradient, and makes share, loss
+ * and slope-weighted results of its frame unspecified.  grad_coef must not overlap coef.
+ *
+ * d->c, d->k unused; H = h * scale, W = w * scale.  `scratch` of sr_select_balance: sr_select_balance_scratch_bytes(d) bytes, 16-byte
+ * aligned, overwritten; two calls that share it must not overlap.  The method's paper has no such loss; it is the usual one of routers
+ * that send each token to s of D experts.
+ */
+size_t sr_select_balance_scratch_bytes(const sr_dims* d);
+int sr_select_balance(const void* coef, int coef_dtype, const uint8_t* idx, const uint8_t* mask, float* loss, int32_t* counts,
+                      float* share, float* slope, const sr_dims* d, int s, uint32_t flags, void* scratch, size_t scratch_bytes,
+                      void* stream);
+int sr_select_balance_grad(const void* coef, int coef_dtype, const uint8_t* mask, const float* slope, const float* grad_loss,
+                           float weight, void* grad_coef, const sr_dims* d, uint32_t flags, void* stream);
+
+/*
+ * sr_adamw_step: one AdamW step (decoupled weight decay) on `count` tensors.  With g = grad * grad_scale, t = step (from 1):
+ *     m = beta1 m + (1 - beta1) g            v = beta2 v + (1 - beta2) g^2
+ *     p = p (1 - lr * weight_decay) - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
+ * in fp32, p rounded to its type.  `tensors` is a HOST array; its pointers are device pointers, aligned to their element sizes
+ * (16 bytes everywhere is faster).  param_dtype, grad_dtype: SR_F32, SR_F16 or SR_BF16, the same for all tensors of a call.
+ *   state_bits = 32: m, v are fp32 [n]; the scale pointers are ignored.
+ *   state_bits = 8:  m and v are one byte an element, e4m3, with one fp32 scale for each 256 consecutive elements (the last
+ *                    block may be shorter): m = m_scale * code, sqrt(v) = v_scale * code.  After the step a block's scale is its
+ *                    largest magnitude / 448 and codes are rounded to nearest even; a root that is not zero is not held as zero
+ *                    (the step would divide by it).  All-zero codes and scales are a fresh state.
+ * A tensor of n = 0 elements is skipped (its pointers may be NULL); tensors of one call must not overlap.
+ * opts (HOST): lr_dev (fp32 [1]), step_dev (int64 [1]) and skip_dev (int32 [1]) are device pointers or NULL; the first two replace lr
+ * and step and the third, where it is not 0, makes the call change nothing, so that a captured step can be replayed with a
+ * schedule, a counter the caller advances, and a found-Inf flag.  A gradient that is not finite gives a parameter and state that
+ * are not finite (8 bits: for its whole block): skip such steps.  The paper names no optimiser; AdamW is the common choice.
+ */
+typedef struct sr_adamw_tensor {
+    void* param;
+    const void* grad;
+    void* m;
+    void* v;
+    float* m_scale;
+    float* v_scale;
+    int64_t n;
+} sr_adamw_tensor;
+typedef struct sr_adamw_opts {
+    double lr, beta1, beta2, eps, weight_decay, grad_scale;
+    int64_t step;
+    const float* lr_dev;
+    const int64_t* step_dev;
+    const int32_t* skip_dev;
+} sr_adamw_opts;
+int sr_adamw_step(const sr_adamw_tensor* tensors, int32_t count, int param_dtype, int grad_dtype, int state_bits,
+                  const sr_adamw_opts* opts, void* stream);
 
 /*
  * Sustained issue rate of an arithmetic pipe of the current device, for the roofline of the kernels that are bound by

@@ -15,15 +15,18 @@ import torch
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libsr.so")
 
-SR_F32, SR_F16 = 0, 1
+SR_F32, SR_F16, SR_BF16 = 0, 1, 2
 SR_CLAMP01, SR_IDX_GLOBAL, SR_COEF_COMPACT, SR_UPSAMPLE_BILINEAR, SR_OUT_F16, SR_OUT_U8, SR_LUMA_ONLY = 1, 2, 4, 8, 16, 32, 64
+SR_GRAD_ADD, SR_BALANCE_PER_FRAME = 128, 256
 SR_OK, SR_ERR_NULL, SR_ERR_SHAPE, SR_ERR_UNSUPPORTED, SR_ERR_ALIGN, SR_ERR_CUDA, SR_ERR_TIMEOUT, SR_ERR_TOO_LARGE = range(8)
 
 EXPORTS = ("sr_bicubic_upsample", "sr_bilinear_upsample", "sr_dict_regress_dense", "sr_dict_select", "sr_dict_regress_selected",
            "sr_status_string", "sr_device_status", "sr_launch_count", "sr_set_wait_limit", "sr_test_lose_arrival", "sr_test_force_kernel",
            "sr_selection_gram", "sr_selection_gram_scratch_bytes", "sr_selection_search", "sr_selection_search_scratch_bytes",
            "sr_selection_gram_static", "sr_probe_rate", "sr_tune_dense", "sr_tune_selected", "sr_tune_reset",
-           "sr_producer_folded_bytes", "sr_producer_fold", "sr_producer_regress")
+           "sr_producer_folded_bytes", "sr_producer_fold", "sr_producer_regress",
+           "sr_dict_regress_grad_scratch_bytes", "sr_dict_regress_dense_grad", "sr_dict_regress_selected_grad",
+           "sr_select_balance_scratch_bytes", "sr_select_balance", "sr_select_balance_grad", "sr_adamw_step")
 
 
 class sr_dims(ctypes.Structure):
@@ -33,6 +36,15 @@ class sr_dims(ctypes.Structure):
 class sr_search_opts(ctypes.Structure):
     _fields_ = [("alpha", ctypes.c_double), ("delta_alpha", ctypes.c_double), ("eps", ctypes.c_double), ("lambda0", ctypes.c_double),
                 ("tol", ctypes.c_double), ("max_sweeps", ctypes.c_int32), ("max_bisect", ctypes.c_int32), ("max_steps", ctypes.c_int32)]
+
+
+class sr_adamw_tensor(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_void_p) for name in ("param", "grad", "m", "v", "m_scale", "v_scale")] + [("n", ctypes.c_int64)]
+
+
+class sr_adamw_opts(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_double) for name in ("lr", "beta1", "beta2", "eps", "weight_decay", "grad_scale")] + \
+               [("step", ctypes.c_int64)] + [(name, ctypes.c_void_p) for name in ("lr_dev", "step_dev", "skip_dev")]
 
 
 class sr_tune_result(ctypes.Structure):
@@ -90,6 +102,15 @@ def load_library() -> ctypes.CDLL:
         lib.sr_producer_folded_bytes.restype = sz
         lib.sr_producer_fold.argtypes = [vp, vp, vp, vp, vp, i32, vp, sz, dp, i32, i32, vp]
         lib.sr_producer_regress.argtypes = [vp, vp, vp, sz, vp, dp, i32, i32, u32, vp]
+        lib.sr_dict_regress_grad_scratch_bytes.argtypes = [dp]
+        lib.sr_dict_regress_grad_scratch_bytes.restype = sz
+        lib.sr_dict_regress_dense_grad.argtypes = [vp, vp, i32, vp, vp, vp, vp, dp, u32, vp, sz, vp]
+        lib.sr_dict_regress_selected_grad.argtypes = [vp, vp, i32, vp, vp, vp, vp, vp, vp, vp, dp, i32, u32, vp, sz, vp]
+        lib.sr_select_balance_scratch_bytes.argtypes = [dp]
+        lib.sr_select_balance_scratch_bytes.restype = sz
+        lib.sr_select_balance.argtypes = [vp, i32, vp, vp, vp, vp, vp, vp, dp, i32, u32, vp, sz, vp]
+        lib.sr_select_balance_grad.argtypes = [vp, i32, vp, vp, vp, ctypes.c_float, vp, dp, u32, vp]
+        lib.sr_adamw_step.argtypes = [ctypes.POINTER(sr_adamw_tensor), i32, i32, i32, i32, ctypes.POINTER(sr_adamw_opts), vp]
         lib.sr_status_string.argtypes = [i32]
         lib.sr_status_string.restype = ctypes.c_char_p
         _lib = lib
@@ -393,3 +414,235 @@ def sr_tune_selected(lr, coef_or_sel, idx, gamma, dict_, scale: int, k: int, s: 
 
 def sr_tune_reset() -> None:
     load_library().sr_tune_reset()
+
+
+def _scratch(nbytes: int, scratch, device, what: str) -> torch.Tensor:
+    """`scratch` checked, or a new buffer of nbytes on `device`."""
+    if nbytes == 0:
+        raise SrError(SR_ERR_UNSUPPORTED, what)
+    if scratch is None:
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
+    return _dev(scratch, torch.uint8, "scratch")
+
+
+def _same_device(first, **others):
+    """All tensors on the current device, whose stream the call runs on."""
+    if _get_device is not None and first.get_device() != _get_device():
+        raise ValueError(f"the tensors are on {first.device}, the current device is cuda:{_get_device()}")
+    for what, t in others.items():
+        if t is not None and t.device != first.device:
+            raise ValueError(f"{what} is on {t.device}, lr or coef on {first.device}")
+
+
+def _grad_out_of(t, shape, dtype, want: bool, like, what: str):
+    """A gradient's buffer: None when it is not wanted, `t` checked, or a new tensor."""
+    if not want:
+        return None
+    if t is None:
+        return torch.empty(shape, dtype=dtype, device=like.device)
+    _dev(t, dtype, what)
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{what} must be {tuple(shape)}")
+    return t
+
+
+def sr_dict_regress_dense_grad(lr, coef, dict_, grad_out, scale: int, k: int, flags: int = 0, grad_coef=None, grad_dict=None,
+                               want_coef: bool = True, want_dict: bool = True, scratch=None):
+    """Gradients of sr_dict_regress_dense for dL/d out = grad_out [n][c][H][W] (float32): (grad_coef, grad_dict), None in the place of one
+    that is not wanted. `scratch`: a uint8 tensor to use instead of allocating one per call."""
+    lr, dict_, grad_out = _dev(lr, torch.float32, "lr"), _dev(dict_, torch.float32, "dict"), _dev(grad_out, torch.float32, "grad_out")
+    code = _coef_code(coef)
+    _dev(coef, coef.dtype, "coef")
+    n, c, h, w = lr.shape
+    D = dict_.shape[0]
+    H, W = h * scale, w * scale
+    if dict_.shape != (D, k * k) or coef.shape != (n, D, H, W) or grad_out.shape != (n, c, H, W):
+        raise ValueError("shapes of lr / coef / dict / grad_out do not agree")
+    _same_device(lr, coef=coef, dict=dict_, grad_out=grad_out, grad_coef=grad_coef, grad_dict=grad_dict, scratch=scratch)
+    grad_coef = _grad_out_of(grad_coef, coef.shape, coef.dtype, want_coef, coef, "grad_coef")
+    grad_dict = _grad_out_of(grad_dict, dict_.shape, torch.float32, want_dict, dict_, "grad_dict")
+    d = sr_dims(n, c, h, w, scale, k, D)
+    lib = _lib or load_library()
+    if want_dict:
+        scratch = _scratch(lib.sr_dict_regress_grad_scratch_bytes(ctypes.byref(d)), scratch, lr.device, "sr_dict_regress_grad_scratch_bytes")
+    status = lib.sr_dict_regress_dense_grad(lr.data_ptr(), coef.data_ptr(), code, dict_.data_ptr(), grad_out.data_ptr(), _ptr(grad_coef),
+                                            _ptr(grad_dict), ctypes.byref(d), flags, _ptr(scratch), 0 if scratch is None else scratch.numel(), _stream())
+    if status:
+        raise SrError(status, "sr_dict_regress_dense_grad")
+    return grad_coef, grad_dict
+
+
+def sr_dict_regress_selected_grad(lr, coef_or_sel, idx, gamma, dict_, grad_out, scale: int, k: int, s: int, flags: int = 0, grad_coef=None,
+                                  grad_dict=None, grad_gamma=None, want_coef: bool = True, want_dict: bool = True, scratch=None):
+    """Gradients of sr_dict_regress_selected with the same idx, gamma and flags: (grad_coef_or_sel, grad_dict, grad_gamma). grad_gamma is
+    None unless gamma is given and want_dict is set."""
+    lr, dict_, grad_out = _dev(lr, torch.float32, "lr"), _dev(dict_, torch.float32, "dict"), _dev(grad_out, torch.float32, "grad_out")
+    code = _coef_code(coef_or_sel)
+    _dev(coef_or_sel, coef_or_sel.dtype, "coef_or_sel")
+    if idx is None:
+        raise ValueError("the gradient needs idx: choose the atoms with sr_dict_select first")
+    _dev(idx, torch.uint8, "idx")
+    if gamma is not None:
+        _dev(gamma, torch.float32, "gamma")
+    n, c, h, w = lr.shape
+    D = dict_.shape[0]
+    H, W = h * scale, w * scale
+    planes = s if (flags & SR_COEF_COMPACT) else D
+    idx_shape = (s,) if (flags & SR_IDX_GLOBAL) else (n, s, H, W)
+    if dict_.shape != (D, k * k) or coef_or_sel.shape != (n, planes, H, W) or grad_out.shape != (n, c, H, W) or idx.shape != idx_shape or \
+            (gamma is not None and gamma.shape != (s,)):
+        raise ValueError("shapes of lr / coef_or_sel / idx / gamma / dict / grad_out do not agree")
+    _same_device(lr, coef_or_sel=coef_or_sel, idx=idx, gamma=gamma, dict=dict_, grad_out=grad_out, grad_coef=grad_coef, grad_dict=grad_dict,
+                 grad_gamma=grad_gamma, scratch=scratch)
+    grad_coef = _grad_out_of(grad_coef, coef_or_sel.shape, coef_or_sel.dtype, want_coef, lr, "grad_coef")
+    grad_dict = _grad_out_of(grad_dict, dict_.shape, torch.float32, want_dict, lr, "grad_dict")
+    grad_gamma = _grad_out_of(grad_gamma, (s,), torch.float32, want_dict and gamma is not None, lr, "grad_gamma")
+    d = sr_dims(n, c, h, w, scale, k, D)
+    lib = _lib or load_library()
+    if want_dict:
+        scratch = _scratch(lib.sr_dict_regress_grad_scratch_bytes(ctypes.byref(d)), scratch, lr.device, "sr_dict_regress_grad_scratch_bytes")
+    status = lib.sr_dict_regress_selected_grad(lr.data_ptr(), coef_or_sel.data_ptr(), code, idx.data_ptr(), _ptr(gamma), dict_.data_ptr(),
+                                               grad_out.data_ptr(), _ptr(grad_coef), _ptr(grad_dict), _ptr(grad_gamma), ctypes.byref(d), s, flags,
+                                               _ptr(scratch), 0 if scratch is None else scratch.numel(), _stream())
+    if status:
+        raise SrError(status, "sr_dict_regress_selected_grad")
+    return grad_coef, grad_dict, grad_gamma
+
+
+def sr_select_balance(coef, idx, mask=None, flags: int = 0, scratch=None):
+    """Balance loss of the selection idx [n][s][H][W] of coef [n][D][H][W]: (loss [1], counts int32 [n][D], share [n][D], slope [n][D]).
+    mask [n][H][W] uint8: pixels with 0 do not count. slope is what sr_select_balance_grad takes."""
+    code = _coef_code(coef)
+    _dev(coef, coef.dtype, "coef"), _dev(idx, torch.uint8, "idx")
+    n, D, H, W = coef.shape
+    s = idx.shape[1] if idx.dim() == 4 else 0
+    if idx.shape != (n, s, H, W) or (mask is not None and _dev(mask, torch.uint8, "mask").shape != (n, H, W)):
+        raise ValueError("shapes of coef / idx / mask do not agree")
+    _same_device(coef, idx=idx, mask=mask, scratch=scratch)
+    d = sr_dims(n, 1, H, W, 1, 1, D)
+    lib = _lib or load_library()
+    scratch = _scratch(lib.sr_select_balance_scratch_bytes(ctypes.byref(d)), scratch, coef.device, "sr_select_balance_scratch_bytes")
+    loss = torch.empty(1, dtype=torch.float32, device=coef.device)
+    counts = torch.empty((n, D), dtype=torch.int32, device=coef.device)
+    share, slope = torch.empty((2, n, D), dtype=torch.float32, device=coef.device)
+    status = lib.sr_select_balance(coef.data_ptr(), code, idx.data_ptr(), _ptr(mask), loss.data_ptr(), counts.data_ptr(), share.data_ptr(),
+                                   slope.data_ptr(), ctypes.byref(d), s, flags, scratch.data_ptr(), scratch.numel(), _stream())
+    if status:
+        raise SrError(status, "sr_select_balance")
+    return loss, counts, share, slope
+
+
+def sr_select_balance_grad(coef, slope, mask=None, weight: float = 1.0, grad_loss=None, flags: int = 0, grad_coef=None) -> torch.Tensor:
+    """weight * grad_loss times the balance loss's gradient with respect to coef (slope from sr_select_balance, the same mask), written
+    to grad_coef or, with SR_GRAD_ADD, added to it."""
+    code = _coef_code(coef)
+    _dev(coef, coef.dtype, "coef"), _dev(slope, torch.float32, "slope")
+    n, D, H, W = coef.shape
+    if slope.shape != (n, D) or (mask is not None and _dev(mask, torch.uint8, "mask").shape != (n, H, W)):
+        raise ValueError("shapes of coef / slope / mask do not agree")
+    if grad_loss is not None and _dev(grad_loss, torch.float32, "grad_loss").numel() != 1:
+        raise ValueError("grad_loss must have one element")
+    if grad_coef is None and (flags & SR_GRAD_ADD):
+        raise ValueError("SR_GRAD_ADD needs grad_coef")
+    _same_device(coef, slope=slope, mask=mask, grad_loss=grad_loss, grad_coef=grad_coef)
+    grad_coef = _grad_out_of(grad_coef, coef.shape, coef.dtype, True, coef, "grad_coef")
+    d = sr_dims(n, 1, H, W, 1, 1, D)
+    status = (_lib or load_library()).sr_select_balance_grad(coef.data_ptr(), code, _ptr(mask), slope.data_ptr(), _ptr(grad_loss), weight,
+                                                             grad_coef.data_ptr(), ctypes.byref(d), flags, _stream())
+    if status:
+        raise SrError(status, "sr_select_balance_grad")
+    return grad_coef
+
+
+ADAMW_BLOCK = 256        # elements that share a scale of the 8-bit states
+_ADAMW_CODES = {torch.float32: SR_F32, torch.float16: SR_F16, torch.bfloat16: SR_BF16}
+
+
+class AdamwPlan:
+    """The tensors of sr_adamw_step, checked once and laid out for the call. Keeps references to them, and follows a tensor whose
+    storage was replaced: every step reads the addresses afresh."""
+
+    def __init__(self, params, exp_avg, exp_avg_sq, avg_scale=None, avg_sq_scale=None):
+        self.params, self.m, self.v = list(params), list(exp_avg), list(exp_avg_sq)
+        eight = avg_scale is not None or avg_sq_scale is not None
+        self.state_bits = 8 if eight else 32
+        self.m_scale, self.v_scale = (list(avg_scale or ()), list(avg_sq_scale or ())) if eight else ([], [])
+        count = len(self.params)
+        if not count or len(self.m) != count or len(self.v) != count or (eight and (len(self.m_scale) != count or len(self.v_scale) != count)):
+            raise ValueError("params, exp_avg, exp_avg_sq (and the scales) must be lists of one length, at least 1")
+        if self.params[0].dtype not in _ADAMW_CODES:
+            raise TypeError("parameters must be float32, float16 or bfloat16")
+        self.device, self.param_dtype = self.params[0].device, self.params[0].dtype
+        self._table = (sr_adamw_tensor * count)()
+        self._held = [self.params, self.m, self.v] + ([self.m_scale, self.v_scale] if eight else [])
+        self._names = ["param", "m", "v"] + (["m_scale", "v_scale"] if eight else [])
+        for i in range(count):
+            self._check(i)
+            self._table[i].n = self.params[i].numel()
+        self._at = [[0] * count for _ in self._held]
+        self._sizes = [p.numel() for p in self.params]
+        self._grad_dtype = None
+
+    def _check(self, i):
+        state = torch.float8_e4m3fn if self.state_bits == 8 else torch.float32
+        n = self.params[i].numel()
+        blocks = (n + ADAMW_BLOCK - 1) // ADAMW_BLOCK
+        _dev(self.params[i], self.param_dtype, f"params[{i}]")
+        parts = [(self.m, state, n, "exp_avg"), (self.v, state, n, "exp_avg_sq")]
+        if self.state_bits == 8:
+            parts += [(self.m_scale, torch.float32, blocks, "avg_scale"), (self.v_scale, torch.float32, blocks, "avg_sq_scale")]
+        for tensors, dtype, size, what in parts:
+            if _dev(tensors[i], dtype, f"{what}[{i}]").numel() != size:
+                raise ValueError(f"{what}[{i}] must have {size} elements")
+            if tensors[i].device != self.device:
+                raise ValueError("all tensors of a plan must be on one device")
+        if self.params[i].device != self.device:
+            raise ValueError("all tensors of a plan must be on one device")
+
+    def _refresh(self):
+        for name, tensors, at in zip(self._names, self._held, self._at):
+            now = [t.data_ptr() for t in tensors]
+            if now != at:
+                for i, (a, b) in enumerate(zip(now, at)):
+                    if a != b:
+                        self._check(i)
+                        if self.params[i].numel() != self._sizes[i]:
+                            raise ValueError(f"params[{i}] changed its size: make a new plan")
+                        setattr(self._table[i], name, a)
+                at[:] = now
+
+
+def sr_adamw_plan(params, exp_avg, exp_avg_sq, avg_scale=None, avg_sq_scale=None) -> AdamwPlan:
+    """A plan for sr_adamw_step over lists of tensors. States: float32 tensors, or (8 bits) float8_e4m3fn tensors with one float32 scale for
+    each ADAMW_BLOCK elements in avg_scale / avg_sq_scale; all zero at the start."""
+    return AdamwPlan(params, exp_avg, exp_avg_sq, avg_scale, avg_sq_scale)
+
+
+def sr_adamw_step(plan: AdamwPlan, grads, step, lr, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, weight_decay: float = 0.01,
+                  grad_scale: float = 1.0, skip=None) -> None:
+    """One AdamW step of the plan's tensors in place. `step` (from 1) and `lr` are numbers or, for a captured step, CUDA tensors of one
+    element (int64, float32); `skip`: int32 CUDA tensor of one element, the step changes nothing where it is not 0."""
+    grads = grads if isinstance(grads, (list, tuple)) else list(grads)
+    _same_device(plan.params[0])
+    if len(grads) != len(plan.params):
+        raise ValueError("one gradient per parameter")
+    dtype, table = grads[0].dtype, plan._table
+    if dtype not in _ADAMW_CODES:
+        raise TypeError("gradients must be float32, float16 or bfloat16")
+    for i, (g, n) in enumerate(zip(grads, plan._sizes)):
+        if g.dtype is not dtype or g.device != plan.device or not g.is_contiguous() or g.numel() != n:
+            raise TypeError(f"grads[{i}] must be a contiguous {dtype} tensor of {n} elements on {plan.device}")
+        table[i].grad = g.data_ptr()
+    plan._refresh()
+    o = sr_adamw_opts(0.0, beta1, beta2, eps, weight_decay, grad_scale, 1, None, None, None)
+    for value, dev_type, host, dev in ((lr, torch.float32, "lr", "lr_dev"), (step, torch.int64, "step", "step_dev"), (skip, torch.int32, None, "skip_dev")):
+        if isinstance(value, torch.Tensor):
+            if _dev(value, dev_type, dev).numel() != 1 or value.device != plan.device:
+                raise ValueError(f"{dev} must have one element, on {plan.device}")
+            setattr(o, dev, value.data_ptr())
+        elif host is not None:
+            setattr(o, host, value)
+        elif value is not None:
+            raise TypeError("skip must be an int32 CUDA tensor")
+    _check((_lib or load_library()).sr_adamw_step(table, len(grads), _ADAMW_CODES[plan.param_dtype], _ADAMW_CODES[dtype], plan.state_bits,
+                                                  ctypes.byref(o), _stream()), "sr_adamw_step")

@@ -15,6 +15,7 @@
 #include "sr_producer.cuh"
 #include "sr_regress_tc.cuh"
 #include "sr_selection.cuh"
+#include "sr_train.cuh"
 #include "sr_umma.cuh"
 
 namespace sr {
@@ -86,7 +87,7 @@ BicubicPhases make_phases(int r, bool bilinear)
     return ph;
 }
 
-static int check_dims(const sr_dims* d, bool need_kD)
+int check_dims(const sr_dims* d, bool need_kD)
 {
     if (!d) return SR_ERR_NULL;
     if (d->n < 1 || d->c < 1 || d->h < 1 || d->w < 1) return SR_ERR_SHAPE;
@@ -104,7 +105,7 @@ static int check_dims(const sr_dims* d, bool need_kD)
     return SR_OK;
 }
 
-static Problem make_problem(const sr_dims* d, int s, uint32_t flags)
+Problem make_problem(const sr_dims* d, int s, uint32_t flags)
 {
     Problem pb{};
     pb.n = d->n; pb.c = d->c; pb.h = d->h; pb.w = d->w; pb.r = d->scale; pb.k = d->k; pb.D = d->D;

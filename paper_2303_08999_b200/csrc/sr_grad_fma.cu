@@ -1,0 +1,448 @@
+// Gradients of the dictionary regression on the fp32 FMA pipe: every shape, fp32 or binary16 coefficients, all modes. The path of
+// fp32 coefficients and the fallback for shapes the tensor-core kernels do not take.
+//
+//   G_j(i)          = sum_c grad_out_c(i) U_c(i + o_j)     per pixel, k*k values, never stored in global memory
+//   grad_coef_l(i)  = sum_j dict[l][j] G_j(i)              grad_coef_kernel: one thread per pixel, G in registers
+//   grad_dict[l][j] = sum_i coef_l(i) G_j(i)               grad_dict_kernel: a product [planes x pixels][pixels x k*k], a
+//                                                          4 x 4 corner of it per thread, pixels staged in shared memory
+// The first writes the coefficient-sized tensor and reads none, the second reads one and writes none, so two kernels move the
+// bytes one would; what they do twice is G (c k^2 multiply-adds a pixel against D k^2).
+#include "sr_train.cuh"
+
+namespace sr {
+
+namespace {
+
+constexpr int TX = 32, CCHUNK = 4;
+
+// The D k^2 multiply-adds of a pixel.
+template <int K> struct KK { static constexpr int value = K * K, padded = (K * K + 3) & ~3; };
+
+// Up-sampled tile of channels c0 .. c0 + nc - 1 with its halo, in shared memory.
+template <int K, int TY>
+__device__ __forceinline__ void fill_u(const float* __restrict__ lr, float* sU, const Problem& pb, int f, int c0, int nc, int X0, int Y0, int tid, int nthr)
+{
+    constexpr int P = (K - 1) / 2, UW = TX + 2 * P, UH = TY + 2 * P;
+    for (int i = tid; i < nc * UH * UW; i += nthr) {
+        const int ch = i / (UH * UW), rem = i - ch * (UH * UW);
+        const int uy = rem / UW, ux = rem - uy * UW;
+        const float* plane = lr + ((int64_t)f * pb.c + c0 + ch) * pb.h * pb.w;
+        sU[i] = bicubic_point(plane, pb.h, pb.w, pb.r, pb.ph, clampi(Y0 - P + uy, 0, pb.H - 1), clampi(X0 - P + ux, 0, pb.W - 1));
+    }
+}
+
+__device__ __forceinline__ void store_coef(float* p, int64_t i, float v) { p[i] = v; }
+__device__ __forceinline__ void store_coef(__half* p, int64_t i, float v) { p[i] = __float2half_rn(v); }
+
+struct CoefGradParams {
+    const float* lr;
+    const uint8_t* idx;
+    const float* gamma;
+    const float* dict;
+    const float* gout;
+    int mode;
+    int tiles_x, tiles_y;
+    Problem pb;
+};
+
+template <int K, typename CoefT>
+__global__ void __launch_bounds__(256)
+grad_coef_kernel(const __grid_constant__ CoefGradParams p, CoefT* __restrict__ gcoef)
+{
+    constexpr int TY = 8, kk = KK<K>::value, kkp = KK<K>::padded, P = (K - 1) / 2;
+    constexpr int UW = TX + 2 * P, UH = TY + 2 * P;
+    extern __shared__ __align__(16) float smem[];
+    __shared__ float sw[256];                    // global subset: the atom's weight
+    __shared__ uint8_t satom[256];               // global subset: the atom of each plane
+    __shared__ uint32_t slisted[8][256];         // lists: which atoms the pixel lists, a bit each
+    const Problem& pb = p.pb;
+    const int D = pb.D, s = pb.s, H = pb.H, W = pb.W;
+    float* sdict = smem;                         // [D][kkp]
+    float* sU = smem + (size_t)D * kkp;          // [CCHUNK][UH][UW]
+    const int tid = threadIdx.y * TX + threadIdx.x;
+    const int per = p.tiles_x * p.tiles_y;
+    const int f = blockIdx.x / per, rest = blockIdx.x - f * per;
+    const int ty = rest / p.tiles_x, tx = rest - ty * p.tiles_x;
+    const int X0 = tx * TX, Y0 = ty * TY, X = X0 + threadIdx.x, Y = Y0 + threadIdx.y;
+    const bool valid = X < W && Y < H;
+    const int64_t HW = (int64_t)H * W;
+    const int64_t pix = (int64_t)min(Y, H - 1) * W + min(X, W - 1);
+    const bool compact = p.mode == kModeCompact || (p.mode == kModeGlobal && (pb.flags & SR_COEF_COMPACT));
+
+    for (int i = tid; i < D * kkp; i += 256) {
+        const int l = i / kkp, j = i - l * kkp;
+        sdict[i] = j < kk ? __ldg(p.dict + (int64_t)l * kk + j) : 0.f;
+    }
+    if (p.mode == kModeGlobal && tid == 0) {
+        for (int l = 0; l < D; ++l) sw[l] = 0.f;
+        for (int q = 0; q < s; ++q) {
+            const int a = min((int)__ldg(p.idx + q), D - 1);
+            const float g = p.gamma ? __ldg(p.gamma + q) : 1.f;
+            satom[q] = (uint8_t)a;
+            if (compact) sw[q] = g;
+            else sw[a] += g;                     // an atom listed twice counts with both weights
+        }
+    }
+    float G[kkp];
+#pragma unroll
+    for (int j = 0; j < kkp; ++j) G[j] = 0.f;
+    for (int c0 = 0; c0 < pb.c; c0 += CCHUNK) {
+        const int nc = min(CCHUNK, pb.c - c0);
+        __syncthreads();
+        fill_u<K, TY>(p.lr, sU, pb, f, c0, nc, X0, Y0, tid, 256);
+        __syncthreads();
+        for (int ch = 0; ch < nc; ++ch) {
+            const float g = valid ? __ldg(p.gout + ((int64_t)f * pb.c + c0 + ch) * HW + pix) : 0.f;
+            const float* u = sU + ch * UH * UW + threadIdx.y * UW + threadIdx.x;
+#pragma unroll
+            for (int a = 0; a < K; ++a)
+#pragma unroll
+                for (int b = 0; b < K; ++b) G[a * K + b] = fmaf(g, u[a * UW + b], G[a * K + b]);
+        }
+    }
+    auto dot = [&](int atom) {
+        const float4* row = reinterpret_cast<const float4*>(sdict + atom * kkp);
+        float acc[4] = {0.f, 0.f, 0.f, 0.f};     // four chains
+#pragma unroll
+        for (int j4 = 0; j4 < kkp / 4; ++j4) {
+            const float4 dv = row[j4];
+            acc[0] = fmaf(dv.x, G[4 * j4 + 0], acc[0]);
+            acc[1] = fmaf(dv.y, G[4 * j4 + 1], acc[1]);
+            acc[2] = fmaf(dv.z, G[4 * j4 + 2], acc[2]);
+            acc[3] = fmaf(dv.w, G[4 * j4 + 3], acc[3]);
+        }
+        return (acc[0] + acc[1]) + (acc[2] + acc[3]);
+    };
+    const int planes = compact ? s : D;
+    CoefT* out = gcoef + (int64_t)f * planes * HW + pix;
+    if (p.mode == kModeCompact) {
+        for (int q = 0; q < s; ++q) {
+            const int a = min((int)__ldg(p.idx + ((int64_t)f * s + q) * HW + pix), D - 1);
+            const float v = dot(a);
+            if (valid) store_coef(out, (int64_t)q * HW, v);
+        }
+    } else if (p.mode == kModeGlobal) {
+        for (int q = 0; q < planes; ++q) {
+            const float w = sw[q];
+            const float v = w != 0.f ? w * dot(compact ? satom[q] : q) : 0.f;
+            if (valid) store_coef(out, (int64_t)q * HW, v);
+        }
+    } else if (p.mode == kModeIdx) {
+        for (int i = 0; i < (D + 31) / 32; ++i) slisted[i][tid] = 0u;
+        for (int q = 0; q < s; ++q) {
+            const int a = min((int)__ldg(p.idx + ((int64_t)f * s + q) * HW + pix), D - 1);
+            slisted[a >> 5][tid] |= 1u << (a & 31);
+        }
+        for (int l = 0; l < D; ++l) {
+            const float v = dot(l);
+            if (valid) store_coef(out, (int64_t)l * HW, (slisted[l >> 5][tid] >> (l & 31)) & 1u ? v : 0.f);
+        }
+    } else {
+        for (int l = 0; l < D; ++l) {
+            const float v = dot(l);
+            if (valid) store_coef(out, (int64_t)l * HW, v);
+        }
+    }
+}
+
+struct DictGradParams {
+    const float* lr;
+    const uint8_t* idx;
+    const float* gout;
+    float* partial;              // [slot][rows][kk]
+    int mode;
+    int rows;                    // planes whose sums are wanted (D, or s of a subset)
+    int chunk;                   // planes a block works on (gridDim.y chunks)
+    int tiles_x, tiles_y, num_tiles;
+    Problem pb;
+};
+
+// A block owns a chunk of planes and walks tiles of 32 x 4 pixels. Per tile: G of every pixel and the planes' coefficients in
+// shared memory, pixels innermost; then thread (row group, tap group, share of the pixels) adds its 4 x 4 corner. The corner of a
+// tile is summed by itself and then added to the running one, so that a long frame adds few numbers of like size.
+template <int K, typename CoefT>
+__global__ void __launch_bounds__(256)
+grad_dict_kernel(const __grid_constant__ DictGradParams p, const CoefT* __restrict__ coef)
+{
+    constexpr int TY = 4, NPX = TX * TY, kk = KK<K>::value, kkp = KK<K>::padded, P = (K - 1) / 2;
+    constexpr int UW = TX + 2 * P, UH = TY + 2 * P;
+    constexpr int PITCH = NPX + 4;               // rows four banks apart: 16-byte reads of eight rows touch every bank once
+    constexpr int TG = kkp / 4;                  // tap groups
+    extern __shared__ __align__(16) float smem[];
+    const Problem& pb = p.pb;
+    const int D = pb.D, s = pb.s, H = pb.H, W = pb.W, tid = threadIdx.x;
+    const int64_t HW = (int64_t)H * W;
+    const int row0 = blockIdx.y * p.chunk, nrow = min(p.chunk, p.rows - row0);
+    const int rgroups = (nrow + 3) / 4, items = rgroups * TG;
+    float* sG = smem;                            // [kkp][PITCH]
+    float* sPhi = sG + kkp * PITCH;              // [chunk rounded up to 4][PITCH]
+    float* sU = sPhi + (size_t)((p.chunk + 3) & ~3) * PITCH;
+    const int shares = max(1, 256 / items);      // threads that split the pixels of one corner
+    const int share = tid / items, item = tid - share * items;
+    const int rg = item / TG, tg = item - rg * TG;
+    const bool works = share < shares;
+
+    for (int i = tid; i < kkp * PITCH; i += 256) sG[i] = 0.f;
+    for (int i = tid; i < ((p.chunk + 3) & ~3) * PITCH; i += 256) sPhi[i] = 0.f;
+    float total[4][4] = {};
+    for (int t = blockIdx.x; t < p.num_tiles; t += gridDim.x) {
+        const int per = p.tiles_x * p.tiles_y;
+        const int f = t / per, rest = t - f * per;
+        const int ty = rest / p.tiles_x, tx = rest - ty * p.tiles_x;
+        const int X0 = tx * TX, Y0 = ty * TY;
+        // ---- the planes' coefficients (zero outside the image)
+        __syncthreads();
+        if (p.mode == kModeIdx || p.mode == kModeCompact) {
+            for (int i = tid; i < nrow * NPX; i += 256) sPhi[(i / NPX) * PITCH + i % NPX] = 0.f;
+            __syncthreads();
+            for (int i = tid; i < s * NPX; i += 256) {
+                const int q = i / NPX, px = i - q * NPX, X = X0 + px % TX, Y = Y0 + px / TX;
+                if (X < W && Y < H) {
+                    const int64_t pix = (int64_t)Y * W + X;
+                    const int a = min((int)__ldg(p.idx + ((int64_t)f * s + q) * HW + pix), D - 1);
+                    if (a >= row0 && a < row0 + nrow)
+                        sPhi[(a - row0) * PITCH + px] = load_coef(coef, (p.mode == kModeCompact ? (int64_t)f * s + q : (int64_t)f * D + a) * HW + pix);
+                }
+            }
+        } else {
+            const bool compact = (pb.flags & SR_COEF_COMPACT) != 0;
+            for (int i = tid; i < nrow * NPX; i += 256) {
+                const int q = i / NPX, px = i - q * NPX, X = X0 + px % TX, Y = Y0 + px / TX;
+                int64_t plane;
+                if (p.mode == kModeGlobal) plane = compact ? (int64_t)f * s + row0 + q : (int64_t)f * D + min((int)__ldg(p.idx + row0 + q), D - 1);
+                else plane = (int64_t)f * D + row0 + q;
+                sPhi[q * PITCH + px] = X < W && Y < H ? load_coef(coef, plane * HW + (int64_t)Y * W + X) : 0.f;
+            }
+        }
+        // ---- G (threads 0 .. NPX - 1, a pixel each)
+        const int px = tid % NPX, half = tid / NPX;              // two threads a pixel, every other patch row each
+        const int gx = X0 + px % TX, gy = Y0 + px / TX;
+        const bool valid = gx < W && gy < H;
+        for (int c0 = 0; c0 < pb.c; c0 += CCHUNK) {
+            const int nc = min(CCHUNK, pb.c - c0);
+            __syncthreads();
+            fill_u<K, TY>(p.lr, sU, pb, f, c0, nc, X0, Y0, tid, 256);
+            __syncthreads();
+            float g[CCHUNK];
+#pragma unroll
+            for (int ch = 0; ch < CCHUNK; ++ch)
+                g[ch] = valid && ch < nc ? __ldg(p.gout + ((int64_t)f * pb.c + c0 + ch) * HW + (int64_t)gy * W + gx) : 0.f;
+            for (int a = half; a < K; a += 2) {
+#pragma unroll
+                for (int b = 0; b < K; ++b) {
+                    float v = c0 == 0 ? 0.f : sG[(a * K + b) * PITCH + px];
+#pragma unroll
+                    for (int ch = 0; ch < CCHUNK; ++ch)
+                        if (ch < nc) v = fmaf(g[ch], sU[(ch * UH + px / TX + a) * UW + px % TX + b], v);
+                    sG[(a * K + b) * PITCH + px] = valid ? v : 0.f;
+                }
+            }
+        }
+        __syncthreads();
+        // ---- the corner
+        if (works) {
+            float acc[4][4] = {};
+            for (int q = share; q < NPX / 4; q += shares) {
+                float4 a[4], b[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) a[i] = *reinterpret_cast<const float4*>(sPhi + (4 * rg + i) * PITCH + 4 * q);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) b[i] = *reinterpret_cast<const float4*>(sG + (4 * tg + i) * PITCH + 4 * q);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        acc[i][j] = fmaf(a[i].w, b[j].w, fmaf(a[i].z, b[j].z, fmaf(a[i].y, b[j].y, fmaf(a[i].x, b[j].x, acc[i][j]))));
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) total[i][j] += acc[i][j];
+        }
+    }
+    // ---- the shares of a corner, one after the other (fixed order), then to the block's slot
+    __syncthreads();
+    float* sum = smem;                           // [items][16]
+    for (int sh = 0; sh < shares; ++sh) {
+        if (share == sh) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) sum[item * 16 + i] = (sh ? sum[item * 16 + i] : 0.f) + total[i / 4][i % 4];
+        }
+        __syncthreads();
+    }
+    if (share == 0) {
+        float* out = p.partial + (int64_t)blockIdx.x * p.rows * kk;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int r = 4 * rg + i / 4, j = 4 * tg + i % 4;
+            if (r < nrow && j < kk) out[(int64_t)(row0 + r) * kk + j] = sum[item * 16 + i];
+        }
+    }
+}
+
+// Sums the slots. A block takes 32 neighbouring elements of one plane row's flat range, eight threads to an element, and adds
+// the eight in a fixed order; fp64, because the partial sums are as large as the whole.
+__global__ void __launch_bounds__(256)
+grad_dict_sum_kernel(const float* __restrict__ partial, int slots, int elems, float* __restrict__ gdict)
+{
+    __shared__ double part[8][33];
+    const int e = blockIdx.x * 32 + threadIdx.x % 32, g = threadIdx.x / 32;
+    double acc = 0.0;
+    if (e < elems) {
+#pragma unroll 8
+        for (int i = g; i < slots; i += 8) acc += (double)__ldg(partial + (int64_t)i * elems + e);
+    }
+    part[g][threadIdx.x % 32] = acc;
+    __syncthreads();
+    if (g == 0 && e < elems) {
+        for (int i = 1; i < 8; ++i) acc += part[i][threadIdx.x];
+        gdict[e] = (float)acc;
+    }
+}
+
+// The same for a subset: block q sums the taps of plane q, writes the re-weight's gradient sum_j dict[a_q][j] A_q[j], and, if it
+// is the first plane of its atom, the atom's row sum of gamma A over the planes of that atom. Blocks s .. s + D - 1 write the
+// zero rows of the atoms outside the subset.
+__global__ void __launch_bounds__(256)
+grad_subset_sum_kernel(const float* __restrict__ partial, int slots, int s, int D, int kk, const uint8_t* __restrict__ idx,
+                       const float* __restrict__ gamma, const float* __restrict__ dict, float* __restrict__ gdict, float* __restrict__ ggamma)
+{
+    __shared__ double part[8][81];
+    __shared__ double rowsum[81];
+    const int tid = threadIdx.x;
+    if ((int)blockIdx.x >= s) {
+        const int l = blockIdx.x - s;
+        bool in = false;
+        for (int q = 0; q < s; ++q) in |= min((int)__ldg(idx + q), D - 1) == l;
+        if (!in && gdict)
+            for (int j = tid; j < kk; j += 256) gdict[(int64_t)l * kk + j] = 0.f;
+        return;
+    }
+    const int q = blockIdx.x, atom = min((int)__ldg(idx + q), D - 1);
+    bool first = true;
+    for (int i = 0; i < q; ++i) first &= min((int)__ldg(idx + i), D - 1) != atom;
+    for (int j = tid; j < kk; j += 256) rowsum[j] = 0.0;
+    for (int q2 = q; q2 < s; ++q2) {
+        if (q2 != q && (!first || !gdict || min((int)__ldg(idx + q2), D - 1) != atom)) continue;
+        __syncthreads();
+        for (int i = tid; i < 8 * kk; i += 256) {
+            const int g = i / kk, j = i - g * kk;
+            double acc = 0.0;
+#pragma unroll 8
+            for (int sl = g; sl < slots; sl += 8) acc += (double)__ldg(partial + ((int64_t)sl * s + q2) * kk + j);
+            part[g][j] = acc;
+        }
+        __syncthreads();
+        if (tid < kk) {
+            double acc = 0.0;
+            for (int g = 0; g < 8; ++g) acc += part[g][tid];
+            part[0][tid] = acc;
+            rowsum[tid] += (gamma ? (double)__ldg(gamma + q2) : 1.0) * acc;
+        }
+        __syncthreads();
+        if (q2 == q && ggamma && tid == 0) {
+            double acc = 0.0;
+            for (int j = 0; j < kk; ++j) acc += (double)__ldg(dict + (int64_t)atom * kk + j) * part[0][j];
+            ggamma[q] = (float)acc;
+        }
+    }
+    __syncthreads();
+    if (first && gdict && tid < kk) gdict[(int64_t)atom * kk + tid] = (float)rowsum[tid];
+}
+
+template <typename Kern> cudaError_t raise_smem(Kern kern, size_t smem)
+{
+    return smem > 48 * 1024 ? cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) : cudaSuccess;
+}
+
+template <int K, typename CoefT> cudaError_t launch_coef_t(const GradArgs& a)
+{
+    constexpr int P = (K - 1) / 2, TY = 8;
+    const Problem& pb = a.pb;
+    CoefGradParams p{a.lr, a.idx, a.gamma, a.dict, a.gout, a.mode, (pb.W + TX - 1) / TX, (pb.H + TY - 1) / TY, pb};
+    const int64_t blocks = (int64_t)p.tiles_x * p.tiles_y * pb.n;
+    if (blocks > 0x7FFFFFFF) return cudaErrorInvalidConfiguration;
+    const size_t smem = ((size_t)pb.D * KK<K>::padded + (size_t)CCHUNK * (TY + 2 * P) * (TX + 2 * P)) * sizeof(float);
+    auto kern = grad_coef_kernel<K, CoefT>;
+    if (cudaError_t e = raise_smem(kern, smem)) return e;
+    kern<<<(unsigned)blocks, dim3(TX, TY), smem, a.st>>>(p, static_cast<CoefT*>(a.gcoef));
+    count_launches(1);
+    return cudaGetLastError();
+}
+
+template <int K, typename CoefT> cudaError_t launch_dict_t(const GradArgs& a, int* slots)
+{
+    constexpr int P = (K - 1) / 2, TY = 4, TG = KK<K>::padded / 4, PITCH = TX * TY + 4;
+    const Problem& pb = a.pb;
+    DictGradParams p{};
+    p.lr = a.lr; p.idx = a.idx; p.gout = a.gout; p.partial = a.scratch; p.mode = a.mode; p.pb = pb;
+    p.rows = grad_rows(a);
+    // planes of a block: at most 256 corners of 4 x 4, and 128 planes (shared memory)
+    constexpr int kMost = 4 * (256 / TG) < 128 ? 4 * (256 / TG) : 128;
+    const int chunks = (p.rows + kMost - 1) / kMost;
+    p.chunk = ((p.rows + chunks - 1) / chunks + 3) & ~3;
+    p.tiles_x = (pb.W + TX - 1) / TX;
+    p.tiles_y = (pb.H + TY - 1) / TY;
+    const int64_t tiles = (int64_t)p.tiles_x * p.tiles_y * pb.n;
+    if (tiles > 0x7FFFFFFF) return cudaErrorInvalidConfiguration;
+    p.num_tiles = (int)tiles;
+    const int gx = (int)(tiles < grad_slots() ? tiles : grad_slots());
+    size_t smem = ((size_t)(KK<K>::padded + p.chunk) * PITCH + (size_t)CCHUNK * (TY + 2 * P) * (TX + 2 * P)) * sizeof(float);
+    const size_t sums = (size_t)((p.chunk + 3) / 4) * TG * 16 * sizeof(float);
+    if (smem < sums) smem = sums;
+    auto kern = grad_dict_kernel<K, CoefT>;
+    if (cudaError_t e = raise_smem(kern, smem)) return e;
+    kern<<<dim3(gx, (p.rows + p.chunk - 1) / p.chunk), 256, smem, a.st>>>(p, static_cast<const CoefT*>(a.coef));
+    count_launches(1);
+    *slots = gx;
+    return cudaGetLastError();
+}
+
+template <typename CoefT> cudaError_t launch_coef_k(const GradArgs& a)
+{
+    switch (a.pb.k) {
+    case 1: return launch_coef_t<1, CoefT>(a);
+    case 3: return launch_coef_t<3, CoefT>(a);
+    case 5: return launch_coef_t<5, CoefT>(a);
+    case 7: return launch_coef_t<7, CoefT>(a);
+    default: return launch_coef_t<9, CoefT>(a);
+    }
+}
+
+template <typename CoefT> cudaError_t launch_dict_k(const GradArgs& a, int* slots)
+{
+    switch (a.pb.k) {
+    case 1: return launch_dict_t<1, CoefT>(a, slots);
+    case 3: return launch_dict_t<3, CoefT>(a, slots);
+    case 5: return launch_dict_t<5, CoefT>(a, slots);
+    case 7: return launch_dict_t<7, CoefT>(a, slots);
+    default: return launch_dict_t<9, CoefT>(a, slots);
+    }
+}
+
+} // namespace
+
+cudaError_t launch_grad_coef_fma(const GradArgs& a)
+{
+    return a.coef_dtype == SR_F16 ? launch_coef_k<__half>(a) : launch_coef_k<float>(a);
+}
+
+cudaError_t launch_grad_dict_fma(const GradArgs& a, int* slots)
+{
+    return a.coef_dtype == SR_F16 ? launch_dict_k<__half>(a, slots) : launch_dict_k<float>(a, slots);
+}
+
+cudaError_t launch_grad_dict_sum(const GradArgs& a, int slots)
+{
+    const int kk = a.pb.k * a.pb.k;
+    if (a.mode == kModeGlobal) {
+        grad_subset_sum_kernel<<<a.pb.s + a.pb.D, 256, 0, a.st>>>(a.scratch, slots, a.pb.s, a.pb.D, kk, a.idx, a.gamma, a.dict, a.gdict, a.ggamma);
+    } else {
+        const int elems = a.pb.D * kk;
+        grad_dict_sum_kernel<<<(elems + 31) / 32, 256, 0, a.st>>>(a.scratch, slots, elems, a.gdict);
+    }
+    count_launches(1);
+    return cudaGetLastError();
+}
+
+} // namespace sr

@@ -1,0 +1,64 @@
+// Launchers of the training-side calls: gradients of the regression, balance loss of a selection, optimiser step.
+#pragma once
+
+#include "sr_common.cuh"
+
+namespace sr {
+
+// Validation and problem set-up shared by the C entry points (sr_api.cu).
+int check_dims(const sr_dims* d, bool need_kD);
+Problem make_problem(const sr_dims* d, int s, uint32_t flags);
+
+// One gradient call. mode: kModeDense, kModeIdx, kModeCompact or kModeGlobal; pb.s = planes of the coefficient gradient that
+// are not zero (D when dense).
+struct GradArgs {
+    int mode;
+    const float* lr;
+    const void* coef;          // may be nullptr when gdict and ggamma are
+    int coef_dtype;
+    const uint8_t* idx;
+    const float* gamma;
+    const float* dict;
+    const float* gout;
+    void* gcoef;               // nullptr: not asked for
+    float* gdict;              // nullptr: not asked for
+    float* ggamma;             // nullptr: not asked for
+    float* scratch;            // partial sums of gdict / ggamma, [slots][planes][k*k]
+    Problem pb;
+    cudaStream_t st;
+};
+
+// Partial sums of the dictionary's gradient that may be in flight: blocks of its kernels, two per multiprocessor.
+inline int grad_slots() { return 2 * sm_count(); }
+// Rows of one partial sum: atoms, or planes of the subset.
+inline int grad_rows(const GradArgs& a) { return a.mode == kModeGlobal ? a.pb.s : a.pb.D; }
+
+// General kernels (sr_grad_fma.cu): every shape and type.
+cudaError_t launch_grad_coef_fma(const GradArgs& a);
+cudaError_t launch_grad_dict_fma(const GradArgs& a, int* slots);      // partial sums only
+// Sums the partial sums of `slots` blocks into gdict and ggamma.
+cudaError_t launch_grad_dict_sum(const GradArgs& a, int slots);
+
+struct BalanceArgs {
+    const void* coef;
+    int coef_dtype;
+    const uint8_t* idx;
+    const uint8_t* mask;
+    float* loss;
+    int32_t* counts;
+    float* share;
+    float* slope;
+    void* scratch;
+    int n, D, s;
+    int64_t HW;
+    bool per_frame;
+    cudaStream_t st;
+};
+size_t balance_scratch_bytes(int n, int D, int64_t HW);
+cudaError_t launch_balance(const BalanceArgs& a);
+cudaError_t launch_balance_grad(const BalanceArgs& a, const float* slope, const float* grad_loss, float weight, void* grad, bool add);
+
+cudaError_t launch_adamw(const sr_adamw_tensor* tensors, int count, int param_dtype, int grad_dtype, int state_bits,
+                         const sr_adamw_opts& o, cudaStream_t st);
+
+} // namespace sr
