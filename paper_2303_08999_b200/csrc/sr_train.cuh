@@ -36,6 +36,11 @@ inline int grad_rows(const GradArgs& a) { return a.mode == kModeGlobal ? a.pb.s 
 // General kernels (sr_grad_fma.cu): every shape and type.
 cudaError_t launch_grad_coef_fma(const GradArgs& a);
 cudaError_t launch_grad_dict_fma(const GradArgs& a, int* slots);      // partial sums only
+// Tensor-core kernels (sr_grad_tc.cu).
+bool grad_coef_tc_supported(const GradArgs& a);
+bool grad_dict_tc_supported(const GradArgs& a);
+cudaError_t launch_grad_coef_tc(const GradArgs& a);
+cudaError_t launch_grad_dict_tc(const GradArgs& a, int* slots);       // partial sums only
 // Sums the partial sums of `slots` blocks into gdict and ggamma.
 cudaError_t launch_grad_dict_sum(const GradArgs& a, int slots);
 

@@ -12,10 +12,10 @@ bool on(const void* p, size_t a) { return ((uintptr_t)p % a) == 0; }
 cudaError_t run_grad(const GradArgs& a)
 {
     if (a.gcoef)
-        if (cudaError_t e = launch_grad_coef_fma(a)) return e;
+        if (cudaError_t e = grad_coef_tc_supported(a) ? launch_grad_coef_tc(a) : launch_grad_coef_fma(a)) return e;
     if (a.gdict || a.ggamma) {
         int slots = 0;
-        if (cudaError_t e = launch_grad_dict_fma(a, &slots)) return e;
+        if (cudaError_t e = grad_dict_tc_supported(a) ? launch_grad_dict_tc(a, &slots) : launch_grad_dict_fma(a, &slots)) return e;
         return launch_grad_dict_sum(a, slots);
     }
     return cudaSuccess;
