@@ -25,14 +25,15 @@ using namespace ptx;
 using namespace tile;
 
 constexpr int kThreads = 256, kGroups = 2, kGroupThreads = 128;
+constexpr int kOutBytes = 16384;                // 128 atoms by 64 pixels on their way to global memory
 constexpr int kMaxTH = 8, kMaxRowsOfGroup = kMaxTH / kGroups, kMaxC = 4;
 
 template <int K> struct GGeo {
     static constexpr int kk = K * K, P = (K - 1) / 2, UW = tile_uw(P);
     static constexpr int BLOCKS = kk > 32 ? 2 : 1;                 // 128-byte columns of a G row: hi | lo side by side, or one each
     static constexpr int LO_CHUNK = kk > 32 ? 0 : 4;               // 16-byte unit where lo starts inside its column
-    static constexpr int CHUNKS = (kk + 7) / 8;                    // 16-byte units that are written
     static constexpr int KSTEPS = (kk + 15) / 16;                  // K-steps of the first product
+    static constexpr int CHUNKS = 2 * KSTEPS;                      // 16-byte units that are written
     static constexpr int G_BYTES = BLOCKS * 128 * 128;
     static constexpr int NB = kk > 32 ? 128 : 64;                  // N of the second product: hi and lo columns
     static constexpr int LO_COL = kk > 32 ? 64 : 32;
@@ -76,6 +77,15 @@ __device__ __forceinline__ bool group_barrier_and(int id, bool pred)
                  : "=r"(r) : "r"((int)pred), "r"(id) : "memory");
     return r != 0;
 }
+// TMA store of a box (innermost coordinate a multiple of eight elements); wait until such stores have read their source, or are done.
+__device__ __forceinline__ void tma_store_4d(const CUtensorMap* map, const void* src, int c0, int c1, int c2, int c3)
+{
+    asm volatile("cp.async.bulk.tensor.4d.global.shared::cta.tile.bulk_group [%0, {%2, %3, %4, %5}], [%1];"
+                 ::"l"((uint64_t)map), "r"(smem_u32(src)), "r"(c0), "r"(c1), "r"(c2), "r"(c3) : "memory");
+}
+__device__ __forceinline__ void bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void bulk_wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
+__device__ __forceinline__ void bulk_wait_all() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 __device__ __forceinline__ void cp_async_wait_all_() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 
 __device__ __forceinline__ unsigned finite_bits(float v) { const unsigned b = __float_as_uint(v) & 0x7FFFFFFFu; return b < 0x7F800000u ? b : 0u; }
@@ -233,24 +243,31 @@ __device__ __forceinline__ Floats carve_floats(uint8_t* at, const GradTcParams& 
 
 // ---- gradient of the coefficients ------------------------------------------------------------------------------------------
 
-// The first product, pixels as rows: accumulator lane = pixel, column = atom. A thread then stores its pixel's value of one plane
-// after the other, 64 bytes a warp, whatever the width's alignment.
-template <int K>
+// The first product in one of two layouts of its result.
+//   ATOMS: accumulator lane = atom, column = pixel (atoms are the rows of the product). A warp puts its 32 atoms' values of 64 pixels
+//          into 4 KB of shared memory (its part of the G tile, which the product has read by then, where the atoms are at most 128) and one TMA store takes them to
+//          their planes; needs W % 8 == 0. Storing a lane's row directly, 32 bytes at a time, touches 32 planes an instruction: 268 us
+//          at 1080p x4, D = 72, where one value of one plane per instruction (below) takes 223.
+//   else:  lane = pixel, column = atom. A thread stores its pixel's value of one plane after the other, 64 bytes a warp, whatever the
+//          alignment.
+template <int K, bool ATOMS>
 __global__ void __launch_bounds__(kThreads, 2)
-grad_coef_tc_kernel(const __grid_constant__ GradTcParams p)
+grad_coef_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ GradTcParams p)
 {
     using G = GGeo<K>;
     extern __shared__ uint8_t smem_raw[];
     __shared__ GradCtl ctl;
     __shared__ float sback[256];                 // 2^e of each plane's atom (0: a plane outside the subset)
-    uint8_t* smem = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+    uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     const Problem& pb = p.g.pb;
     const int tid = threadIdx.x, grp = tid / kGroupThreads, x = tid % kGroupThreads, lane = tid & 31, warp = tid >> 5;
     const int C = pb.c, D = pb.D, W = pb.W, rows_pad = (p.rows + 15) & ~15;
     uint8_t* sG = smem + grp * G::G_BYTES;
     uint8_t* sD = smem + kGroups * G::G_BYTES;   // [column][rows_pad][128 B]
     const int d_block = rows_pad * 128;
-    const Floats s = carve_floats(sD + G::BLOCKS * d_block, p, G::UW);
+    // results on their way out: in the G tile, or, where a second product of the same row still reads that, behind the atoms
+    uint8_t* sOut = ATOMS && p.rows > 128 ? sD + G::BLOCKS * d_block + grp * kOutBytes : sG;
+    const Floats s = carve_floats(sD + G::BLOCKS * d_block + (ATOMS && p.rows > 128 ? kGroups * kOutBytes : 0), p, G::UW);
 
     init_ctl(ctl, p, tid);
     for (int i = tid; i < (kGroups * G::G_BYTES + G::BLOCKS * d_block) / 16; i += kThreads) reinterpret_cast<uint4*>(smem)[i] = make_uint4(0, 0, 0, 0);
@@ -291,7 +308,6 @@ grad_coef_tc_kernel(const __grid_constant__ GradTcParams p)
     const uint32_t tmem = ctl.tmem_base + grp * 128;
     volatile WaitCtx* wc = &ctl.wait;
     const int64_t HW = (int64_t)pb.H * W;
-    const bool lists = p.mode == kModeIdx || p.mode == kModeCompact;
     const uint64_t g_desc = make_smem_desc(smem_u32(sG), 16, 1024, kSwizzle128B);
     const uint64_t d_desc = make_smem_desc(smem_u32(sD), 16, 1024, kSwizzle128B);
     constexpr uint32_t kGLo = (G::BLOCKS == 2 ? 128 * 128 : G::LO_CHUNK * 16) >> 4;
@@ -307,6 +323,10 @@ grad_coef_tc_kernel(const __grid_constant__ GradTcParams p)
         for (int row = grp; row < w.rows; row += kGroups) {
             float v[G::kk];
             patch_grad<K>(s.U + row * G::UW + x, p.g.uh * G::UW, s.g + row * C * kGroupThreads + x, C, ts.scale, v);
+            if (ATOMS) {                         // every warp's stores have read the tile
+                if (lane == 0) bulk_wait_read();
+                ok = group_barrier_and(1 + grp, ok);
+            }
             write_row<K>(sG, 128 * 128, x, v);
             const int64_t pix = (int64_t)(w.y0 + row) * W + w.x0 + x;
             bool go = true;                      // the group's: a thread leaves only where all do
@@ -318,13 +338,14 @@ grad_coef_tc_kernel(const __grid_constant__ GradTcParams p)
                 if (!go) break;
                 if (x == 0) {
                     tc_fence_after_sync();
-                    const uint32_t idesc = make_idesc_f16(128, (nr + 15) & ~15, false, false);
+                    const uint32_t idesc = make_idesc_f16(128, ATOMS ? 128 : (nr + 15) & ~15, false, false);
                     const uint64_t dd = d_desc + (uint64_t)((uint32_t)m0 * 128u >> 4);
 #pragma unroll
                     for (int ks = 0; ks < G::KSTEPS; ++ks) {
-                        mma_f16_ss(tmem, g_desc + 2 * ks, dd + 2 * ks, idesc, ks > 0);
-                        mma_f16_ss(tmem, g_desc + kGLo + 2 * ks, dd + 2 * ks, idesc, 1u);
-                        mma_f16_ss(tmem, g_desc + 2 * ks, dd + kDLo + 2 * ks, idesc, 1u);
+                        const uint64_t gh = g_desc + 2 * ks, gl = gh + kGLo, dh = dd + 2 * ks, dl = dh + kDLo;
+                        mma_f16_ss(tmem, ATOMS ? dh : gh, ATOMS ? gh : dh, idesc, ks > 0);
+                        mma_f16_ss(tmem, ATOMS ? dh : gl, ATOMS ? gl : dh, idesc, 1u);
+                        mma_f16_ss(tmem, ATOMS ? dl : gh, ATOMS ? gh : dl, idesc, 1u);
                     }
                     if (lose) lose = false;
                     else mma_commit(&ctl.mma[grp]);
@@ -334,17 +355,56 @@ grad_coef_tc_kernel(const __grid_constant__ GradTcParams p)
                 phase ^= 1;
                 tc_fence_after_sync();
                 if (!ok) continue;               // (the next barrier tells the group)
-                if (!lists) {
+                const uint32_t at = tmem + ((uint32_t)(32 * (warp & 3)) << 16);
+                if (ATOMS) {
+                    const int l = 32 * (warp & 3) + lane;
+                    if (l - lane < nr) {
+                        const float back = l < nr ? sback[m0 + l] : 0.f, k = back * ts.unscale;
+                        uint8_t* mine = sOut + (warp & 3) * (kOutBytes / 4);
+#pragma unroll
+                        for (int c0 = 0; c0 < 128; c0 += 64) {
+                            uint32_t h[32];
+#pragma unroll
+                            for (int c1 = 0; c1 < 64; c1 += 32) {
+                                float acc[32];
+                                tmem_ld_x16(at + c0 + c1, acc);
+                                tmem_ld_x16(at + c0 + c1 + 16, acc + 16);
+                                tmem_ld_wait();
+#pragma unroll
+                                for (int i = 0; i < 16; ++i) {
+                                    const __half2 v2 = __floats2half2_rn(acc[2 * i] * k, acc[2 * i + 1] * k);
+                                    h[c1 / 2 + i] = back != 0.f ? *reinterpret_cast<const uint32_t*>(&v2) : 0u;
+                                }
+                            }
+                            if (c0 > 0 || m0 > 0) {                          // the store before has read the buffer
+                                if (lane == 0) bulk_wait_read();
+                                __syncwarp();
+                            }
+#pragma unroll
+                            for (int j = 0; j < 8; ++j)
+                                *reinterpret_cast<uint4*>(mine + lane * 128 + ((j ^ (lane & 7)) << 4)) = make_uint4(h[4 * j], h[4 * j + 1], h[4 * j + 2], h[4 * j + 3]);
+                            fence_proxy_async_smem();
+                            __syncwarp();
+                            if (lane == 0 && w.x0 + c0 < W) {
+                                tma_store_4d(&map, mine, w.x0 + c0, w.y0 + row, m0 + l, w.f);
+                                bulk_commit();
+                            }
+                        }
+                    }
+                } else {
                     __half* out = p.gcoef + ((int64_t)w.f * p.planes + m0) * HW + pix;
                     for (int l0 = 0; l0 < nr; l0 += 16) {
                         float acc[16];
-                        tmem_ld_x16(tmem + ((uint32_t)(32 * (warp & 3)) << 16) + l0, acc);
+                        tmem_ld_x16(at + l0, acc);
                         tmem_ld_wait();
+                        if (inside) {
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            if (l0 + i < nr && inside) {
-                                const float back = sback[m0 + l0 + i];
-                                out[(int64_t)(l0 + i) * HW] = __float2half_rn(back != 0.f ? acc[i] * ts.unscale * back : 0.f);
+                            for (int i = 0; i < 16; ++i) {
+                                if (l0 + i < nr) {
+                                    const float back = sback[m0 + l0 + i];
+                                    *out = __float2half_rn(back != 0.f ? acc[i] * (back * ts.unscale) : 0.f);
+                                    out += HW;
+                                }
                             }
                         }
                     }
@@ -353,7 +413,8 @@ grad_coef_tc_kernel(const __grid_constant__ GradTcParams p)
             if (!go) { ok = false; break; }
         }
     }
-    // ---- teardown: every product finished before tensor memory is freed
+    // ---- teardown: every product finished before tensor memory is freed, every store before shared memory is
+    if (ATOMS && lane == 0) bulk_wait_all();
     if (x == 0) { mma_commit(&ctl.drain); mbar_wait_drain(&ctl.drain, 0); }
     __syncwarp();
     cp_async_wait_all_();
@@ -362,7 +423,6 @@ grad_coef_tc_kernel(const __grid_constant__ GradTcParams p)
     tc_fence_after_sync();
     if (ctl.wait.abort_flag && tid == 0) atomicExch(p.status, SR_ERR_TIMEOUT);
     if (warp == 0) tmem_dealloc(ctl.tmem_base, kGroups * 128);
-    (void)lane;
 }
 
 // ---- gradient of the dictionary --------------------------------------------------------------------------------------------
@@ -377,7 +437,7 @@ grad_dict_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_consta
     constexpr int TMEM_COLS = kGroups * MB * G::NB;
     extern __shared__ uint8_t smem_raw[];
     __shared__ GradCtl ctl;
-    uint8_t* smem = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+    uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     const Problem& pb = p.g.pb;
     const int tid = threadIdx.x, grp = tid / kGroupThreads, x = tid % kGroupThreads, lane = tid & 31, warp = tid >> 5;
     const int C = pb.c, D = pb.D, W = pb.W, s_ = pb.s;
@@ -625,9 +685,29 @@ int blocks_per_sm(size_t smem) { return 2 * (smem + kStaticReserve) <= (size_t)s
 
 int coef_rows(const GradArgs& a) { return a.mode == kModeGlobal && (a.pb.flags & SR_COEF_COMPACT) ? a.pb.s : a.pb.D; }
 
+// A [n][planes][H][W] binary16 tensor in boxes of 64 pixels of one row by `box_planes` planes, 128-byte swizzle.
+bool encode_planes(CUtensorMap* map, const void* base, const Problem& pb, int planes, int box_planes)
+{
+    const cuuint64_t dims[4] = {(cuuint64_t)pb.W, (cuuint64_t)pb.H, (cuuint64_t)planes, (cuuint64_t)pb.n};
+    const cuuint64_t strides[3] = {(cuuint64_t)pb.W * 2, (cuuint64_t)pb.W * pb.H * 2, (cuuint64_t)pb.W * pb.H * 2 * planes};
+    const cuuint32_t es[4] = {1, 1, 1, 1}, box[4] = {64, 1, (cuuint32_t)box_planes, 1};
+    return encode_fn() && encode_fn()(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, const_cast<void*>(base), dims, strides, box, es,
+                                      CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                                      CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Plane rows that TMA can store.
+bool coef_atoms(const GradArgs& a) { return a.pb.W % 8 == 0 && ((uintptr_t)a.gcoef & 15) == 0 && encode_fn(); }
+
 template <int K> size_t coef_smem(Geom& g, const GradArgs& a)
 {
-    return 1024 + kGroups * GGeo<K>::G_BYTES + (size_t)GGeo<K>::BLOCKS * ((coef_rows(a) + 15) & ~15) * 128 + float_bytes<K>(g, a.pb, a.lr);
+    const int rows_pad = (coef_rows(a) + 15) & ~15;
+    const size_t before = 1024 + kGroups * GGeo<K>::G_BYTES;
+    const size_t all = before + (size_t)GGeo<K>::BLOCKS * rows_pad * 128 + (rows_pad > 128 && coef_atoms(a) ? kGroups * kOutBytes : 0) +
+                       float_bytes<K>(g, a.pb, a.lr);
+    // atoms as rows: the product reads them 128 at a time, whatever lies behind the last one must be shared memory
+    const size_t reach = before + (size_t)(GGeo<K>::BLOCKS - 1) * rows_pad * 128 + (size_t)((rows_pad + 127) / 128) * 128 * 128;
+    return all > reach ? all : reach;
 }
 
 int stage_bytes_of(int rows) { return 2 * ((rows + 7) & ~7) * 128; }
@@ -658,19 +738,23 @@ GradTcParams common_params(const GradArgs& a)
     return p;
 }
 
-template <int K> cudaError_t launch_coef_k(const GradArgs& a)
+template <int K, bool ATOMS> cudaError_t launch_coef_ka(const GradArgs& a)
 {
     GradTcParams p = common_params(a);
     if (!p.status) return cudaErrorUnknown;
     const size_t smem = coef_smem<K>(p.g, a);
     p.rows = coef_rows(a);
+    CUtensorMap map{};
+    if (ATOMS && !encode_planes(&map, a.gcoef, a.pb, p.planes, 32)) return cudaErrorUnknown;
     static bool done[64] = {false};
-    if (cudaError_t e = allow_smem(grad_coef_tc_kernel<K>, done)) return e;
+    if (cudaError_t e = allow_smem(grad_coef_tc_kernel<K, ATOMS>, done)) return e;
     const int most = sm_count() * blocks_per_sm(smem);
-    grad_coef_tc_kernel<K><<<p.g.num_tiles < most ? p.g.num_tiles : most, kThreads, smem, a.st>>>(p);
+    grad_coef_tc_kernel<K, ATOMS><<<p.g.num_tiles < most ? p.g.num_tiles : most, kThreads, smem, a.st>>>(map, p);
     count_launches(1);
     return cudaGetLastError();
 }
+
+template <int K> cudaError_t launch_coef_k(const GradArgs& a) { return coef_atoms(a) ? launch_coef_ka<K, true>(a) : launch_coef_ka<K, false>(a); }
 
 template <int K, int MB> cudaError_t launch_dict_km(const GradArgs& a, int* slots)
 {
@@ -683,14 +767,7 @@ template <int K, int MB> cudaError_t launch_dict_km(const GradArgs& a, int* slot
     CUtensorMap map{};
     const Problem& pb = a.pb;
     const bool whole = a.mode == kModeDense || (a.mode == kModeGlobal && (pb.flags & SR_COEF_COMPACT));
-    if (whole && pb.W % 8 == 0 && ((uintptr_t)a.coef & 15) == 0 && encode_fn()) {
-        const cuuint64_t dims[4] = {(cuuint64_t)pb.W, (cuuint64_t)pb.H, (cuuint64_t)p.planes, (cuuint64_t)pb.n};
-        const cuuint64_t strides[3] = {(cuuint64_t)pb.W * 2, (cuuint64_t)pb.W * pb.H * 2, (cuuint64_t)pb.W * pb.H * 2 * p.planes};
-        const cuuint32_t es[4] = {1, 1, 1, 1}, box[4] = {64, 1, (cuuint32_t)p.rows, 1};
-        p.tma = encode_fn()(&map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, const_cast<void*>(a.coef), dims, strides, box, es,
-                            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-    }
+    p.tma = whole && pb.W % 8 == 0 && ((uintptr_t)a.coef & 15) == 0 && encode_planes(&map, a.coef, pb, p.planes, p.rows);
     static bool done[64] = {false};
     if (cudaError_t e = allow_smem(grad_dict_tc_kernel<K, MB>, done)) return e;
     const int most = sm_count() * (MB == 1 ? blocks_per_sm(smem) : 1);
