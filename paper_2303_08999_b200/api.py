@@ -10,6 +10,7 @@ from __future__ import annotations
 import ctypes
 import os
 
+import numpy
 import torch
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -559,8 +560,9 @@ _ADAMW_CODES = {torch.float32: SR_F32, torch.float16: SR_F16, torch.bfloat16: SR
 
 
 class AdamwPlan:
-    """The tensors of sr_adamw_step, checked once and laid out for the call. Keeps references to them, and follows a tensor whose
-    storage was replaced: every step reads the addresses afresh."""
+    """The tensors of sr_adamw_step, checked once and laid out for the call. A parameter whose storage was replaced (p.data = ...) is
+    followed: every step reads the parameters' addresses afresh. The states belong to the plan while it lives: change them in place,
+    or make a new plan (it keeps their memory, so a state that was given other storage is not followed but stays valid)."""
 
     def __init__(self, params, exp_avg, exp_avg_sq, avg_scale=None, avg_sq_scale=None):
         self.params, self.m, self.v = list(params), list(exp_avg), list(exp_avg_sq)
@@ -574,14 +576,17 @@ class AdamwPlan:
             raise TypeError("parameters must be float32, float16 or bfloat16")
         self.device, self.param_dtype = self.params[0].device, self.params[0].dtype
         self._table = (sr_adamw_tensor * count)()
-        self._held = [self.params, self.m, self.v] + ([self.m_scale, self.v_scale] if eight else [])
-        self._names = ["param", "m", "v"] + (["m_scale", "v_scale"] if eight else [])
+        self._columns = numpy.frombuffer(self._table, dtype=numpy.uint64).reshape(count, 7)      # param, grad, m, v, m_scale, v_scale, n
+        self._states = [[t.detach() for t in tensors] for tensors in (self.m, self.v, self.m_scale, self.v_scale)]     # own references to the memory
         for i in range(count):
             self._check(i)
-            self._table[i].n = self.params[i].numel()
-        self._at = [[0] * count for _ in self._held]
+        for column, tensors in zip((2, 3, 4, 5), self._states):
+            if tensors:
+                self._columns[:, column] = [t.data_ptr() for t in tensors]
         self._sizes = [p.numel() for p in self.params]
-        self._grad_dtype = None
+        self._columns[:, 6] = self._sizes
+        self._at = [p.data_ptr() for p in self.params]
+        self._columns[:, 0] = self._at
 
     def _check(self, i):
         state = torch.float8_e4m3fn if self.state_bits == 8 else torch.float32
@@ -599,17 +604,15 @@ class AdamwPlan:
         if self.params[i].device != self.device:
             raise ValueError("all tensors of a plan must be on one device")
 
-    def _refresh(self):
-        for name, tensors, at in zip(self._names, self._held, self._at):
-            now = [t.data_ptr() for t in tensors]
-            if now != at:
-                for i, (a, b) in enumerate(zip(now, at)):
-                    if a != b:
-                        self._check(i)
-                        if self.params[i].numel() != self._sizes[i]:
-                            raise ValueError(f"params[{i}] changed its size: make a new plan")
-                        setattr(self._table[i], name, a)
-                at[:] = now
+    def _follow(self, at):
+        """Parameters whose address is another than at the last step."""
+        for i, (a, b) in enumerate(zip(at, self._at)):
+            if a != b:
+                self._check(i)
+        if [p.numel() for p in self.params] != self._sizes:
+            raise ValueError("a parameter changed its size: make a new plan")
+        self._at = at
+        self._columns[:, 0] = at
 
 
 def sr_adamw_plan(params, exp_avg, exp_avg_sq, avg_scale=None, avg_sq_scale=None) -> AdamwPlan:
@@ -629,11 +632,15 @@ def sr_adamw_step(plan: AdamwPlan, grads, step, lr, beta1: float = 0.9, beta2: f
     dtype, table = grads[0].dtype, plan._table
     if dtype not in _ADAMW_CODES:
         raise TypeError("gradients must be float32, float16 or bfloat16")
-    for i, (g, n) in enumerate(zip(grads, plan._sizes)):
-        if g.dtype is not dtype or g.device != plan.device or not g.is_contiguous() or g.numel() != n:
-            raise TypeError(f"grads[{i}] must be a contiguous {dtype} tensor of {n} elements on {plan.device}")
-        table[i].grad = g.data_ptr()
-    plan._refresh()
+    # (whole lists at a time: with many small tensors the step is as long as these lines)
+    tensor = torch.Tensor
+    if {g.dtype for g in grads} != {dtype} or set(map(tensor.get_device, grads)) != {plan.device.index} or \
+            not all(map(tensor.is_contiguous, grads)) or list(map(tensor.numel, grads)) != plan._sizes:
+        raise TypeError(f"grads must be contiguous {dtype} tensors on {plan.device}, of their parameters' sizes")
+    plan._columns[:, 1] = list(map(tensor.data_ptr, grads))
+    at = list(map(tensor.data_ptr, plan.params))
+    if at != plan._at:
+        plan._follow(at)
     o = sr_adamw_opts(0.0, beta1, beta2, eps, weight_decay, grad_scale, 1, None, None, None)
     for value, dev_type, host, dev in ((lr, torch.float32, "lr", "lr_dev"), (step, torch.int64, "step", "step_dev"), (skip, torch.int32, None, "skip_dev")):
         if isinstance(value, torch.Tensor):

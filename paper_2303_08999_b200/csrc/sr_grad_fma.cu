@@ -287,6 +287,7 @@ grad_dict_sum_kernel(const float* __restrict__ partial, int slots, int elems, fl
 {
     __shared__ double part[8][33];
     const int e = blockIdx.x * 32 + threadIdx.x % 32, g = threadIdx.x / 32;
+    wait_for_launch_before();
     double acc = 0.0;
     if (e < elems) {
 #pragma unroll 8
@@ -310,6 +311,7 @@ grad_subset_sum_kernel(const float* __restrict__ partial, int slots, int s, int 
     __shared__ double part[8][81];
     __shared__ double rowsum[81];
     const int tid = threadIdx.x;
+    wait_for_launch_before();
     if ((int)blockIdx.x >= s) {
         const int l = blockIdx.x - s;
         bool in = false;
@@ -435,14 +437,12 @@ cudaError_t launch_grad_dict_fma(const GradArgs& a, int* slots)
 cudaError_t launch_grad_dict_sum(const GradArgs& a, int slots)
 {
     const int kk = a.pb.k * a.pb.k;
-    if (a.mode == kModeGlobal) {
-        grad_subset_sum_kernel<<<a.pb.s + a.pb.D, 256, 0, a.st>>>(a.scratch, slots, a.pb.s, a.pb.D, kk, a.idx, a.gamma, a.dict, a.gdict, a.ggamma);
-    } else {
-        const int elems = a.pb.D * kk;
-        grad_dict_sum_kernel<<<(elems + 31) / 32, 256, 0, a.st>>>(a.scratch, slots, elems, a.gdict);
-    }
+    const float* partial = a.scratch;
     count_launches(1);
-    return cudaGetLastError();
+    if (a.mode == kModeGlobal)
+        return launch_after(grad_subset_sum_kernel, dim3(a.pb.s + a.pb.D), 256, a.st, partial, slots, a.pb.s, a.pb.D, kk, a.idx, a.gamma, a.dict, a.gdict, a.ggamma);
+    const int elems = a.pb.D * kk;
+    return launch_after(grad_dict_sum_kernel, dim3((elems + 31) / 32), 256, a.st, partial, slots, elems, a.gdict);
 }
 
 } // namespace sr

@@ -66,4 +66,24 @@ cudaError_t launch_balance_grad(const BalanceArgs& a, const float* slope, const 
 cudaError_t launch_adamw(const sr_adamw_tensor* tensors, int count, int param_dtype, int grad_dtype, int state_bits,
                          const sr_adamw_opts& o, cudaStream_t st);
 
+#ifdef __CUDACC__
+// A kernel that sums what the launch before it on the stream wrote: it may be brought up while that one ends (programmatic dependent
+// launch) and waits for its end, with all it wrote, in wait_for_launch_before().
+template <typename... Params, typename... Args>
+cudaError_t launch_after(void (*kern)(Params...), dim3 grid, int threads, cudaStream_t st, Args... args)
+{
+    cudaLaunchAttribute attr{};
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.stream = st;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kern, static_cast<Params>(args)...);
+}
+__device__ __forceinline__ void wait_for_launch_before() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+#endif
+
 } // namespace sr
