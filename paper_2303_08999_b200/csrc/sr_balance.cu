@@ -7,6 +7,8 @@
 // their magnitudes; the warps' sums meet in shared memory, where one thread a pixel finishes them; then every warp works on from its
 // registers, so the planes are read from memory once although a share needs the whole column first. Widening costs an instruction
 // an element, so magnitudes and signs are taken on the packed words.
+#include <type_traits>
+
 #include "sr_train.cuh"
 
 namespace sr {
@@ -15,54 +17,64 @@ namespace {
 
 constexpr float kSmallestNormal = 1.17549435e-38f;
 
-// A lane's share of one atom of a tile: four 32-bit words, PX pixels. VEC: neighbouring pixels, one 16-byte access (planes and bases
-// that allow it); else the words' elements are 32 pixels apart, so that single-element accesses of a warp are one run.
+// A lane's share of one atom of a tile: four 32-bit words. VEC: neighbouring pixels, one 16-byte access (planes and bases that allow it); else the words' elements are 32 pixels apart, so that single-element accesses of a warp are one run.
 template <typename CoefT> struct Lane;
 template <> struct Lane<float> {
-    static constexpr int PX = 4;
+    static constexpr int PER = 1;                // pixels of a word
     static constexpr uint32_t kMagnitude = 0x7FFFFFFFu;
-    static __device__ __forceinline__ float get(const uint32_t (&v)[4], int i) { return __uint_as_float(v[i]); }
+    static __device__ __forceinline__ float get(const uint32_t* v, int i) { return __uint_as_float(v[i]); }
+    static __device__ __forceinline__ float add(const uint32_t* v, int i, float s) { return s + __uint_as_float(v[i]); }
     static __device__ __forceinline__ uint32_t one(const float* p) { return __float_as_uint(__ldcs(p)); }
-    static __device__ __forceinline__ void put(uint32_t (&v)[4], int i, uint32_t x) { v[i] = x; }
-    static __device__ __forceinline__ uint32_t keep(const bool (&on)[4], int j) { return on[j] ? kMagnitude : 0u; }
+    static __device__ __forceinline__ void put(uint32_t* v, int i, uint32_t x) { v[i] = x; }
+    static __device__ __forceinline__ uint32_t keep(const bool* on, int j) { return on[j] ? kMagnitude : 0u; }
 };
 template <> struct Lane<__half> {
-    static constexpr int PX = 8;
+    static constexpr int PER = 2;
     static constexpr uint32_t kMagnitude = 0x7FFF7FFFu;
-    static __device__ __forceinline__ float get(const uint32_t (&v)[4], int i)
+    static __device__ __forceinline__ float get(const uint32_t* v, int i)
     {
         const __half2 h = *reinterpret_cast<const __half2*>(&v[i / 2]);
         return i % 2 ? __high2float(h) : __low2float(h);
     }
+    // s + element i: the addition that takes a binary16 operand
+    static __device__ __forceinline__ float add(const uint32_t* v, int i, float s)
+    {
+        float d;
+        if (i % 2) asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %1;\n\tadd.f32.f16 %0, b, %2;\n\t}" : "=f"(d) : "r"(v[i / 2]), "f"(s));
+        else asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %1;\n\tadd.f32.f16 %0, a, %2;\n\t}" : "=f"(d) : "r"(v[i / 2]), "f"(s));
+        return d;
+    }
     static __device__ __forceinline__ uint32_t one(const __half* p) { return (uint32_t)__half_as_ushort(__ldcs(p)); }
-    static __device__ __forceinline__ void put(uint32_t (&v)[4], int i, uint32_t x) { v[i / 2] = i % 2 ? __byte_perm(v[i / 2], x, 0x5410) : x; }
-    static __device__ __forceinline__ uint32_t keep(const bool (&on)[8], int j) { return (on[2 * j] ? 0x7FFFu : 0u) | (on[2 * j + 1] ? 0x7FFF0000u : 0u); }
+    static __device__ __forceinline__ void put(uint32_t* v, int i, uint32_t x) { v[i / 2] = i % 2 ? __byte_perm(v[i / 2], x, 0x5410) : x; }
+    static __device__ __forceinline__ uint32_t keep(const bool* on, int j) { return (on[2 * j] ? 0x7FFFu : 0u) | (on[2 * j + 1] ? 0x7FFF0000u : 0u); }
 };
 
 template <int PX, bool VEC> __device__ __forceinline__ int slot_pixel(int lane, int i) { return VEC ? lane * PX + i : lane + 32 * i; }
 
+constexpr int NW = 4;                            // words of a lane
+__device__ __forceinline__ void unpack(uint32_t* x, const uint4& t) { x[0] = t.x; x[1] = t.y; x[2] = t.z; x[3] = t.w; }
+
 // The tile's words of this warp's atoms; zero beyond the frame's end.
 template <typename CoefT, int AW, int WARPS, bool VEC>
-__device__ __forceinline__ void load_words(uint32_t (&x)[AW][4], const CoefT* tile, int64_t HW, int left, int D, int warp, int lane)
+__device__ __forceinline__ void load_words(uint32_t (&x)[AW][NW], const CoefT* tile, int64_t HW, int left, int D, int warp, int lane)
 {
     using L = Lane<CoefT>;
-    const CoefT* src = tile + (int64_t)warp * HW + (VEC ? lane * L::PX : lane);
-    const bool whole = left >= 32 * L::PX;
+    constexpr int PX = NW * L::PER;
+    const CoefT* src = tile + (int64_t)warp * HW + (VEC ? lane * PX : lane);
+    const bool whole = left >= 32 * PX;
 #pragma unroll
     for (int a = 0; a < AW; ++a, src += WARPS * HW) {
-        x[a][0] = x[a][1] = x[a][2] = x[a][3] = 0u;
+#pragma unroll
+        for (int j = 0; j < NW; ++j) x[a][j] = 0u;
         if (warp + a * WARPS < D) {
             if (VEC) {
-                if (lane * L::PX < left) {
-                    const uint4 t = __ldcs(reinterpret_cast<const uint4*>(src));
-                    x[a][0] = t.x; x[a][1] = t.y; x[a][2] = t.z; x[a][3] = t.w;
-                }
+                if (lane * PX < left) unpack(x[a], __ldcs(reinterpret_cast<const uint4*>(src)));
             } else if (whole) {
 #pragma unroll
-                for (int i = 0; i < L::PX; ++i) L::put(x[a], i, L::one(src + 32 * i));
+                for (int i = 0; i < PX; ++i) L::put(x[a], i, L::one(src + 32 * i));
             } else {
 #pragma unroll
-                for (int i = 0; i < L::PX; ++i) L::put(x[a], i, lane + 32 * i < left ? L::one(src + 32 * i) : 0u);
+                for (int i = 0; i < PX; ++i) L::put(x[a], i, lane + 32 * i < left ? L::one(src + 32 * i) : 0u);
             }
         }
     }
@@ -70,28 +82,32 @@ __device__ __forceinline__ void load_words(uint32_t (&x)[AW][4], const CoefT* ti
 
 // What to keep of each word: its magnitude bits, nothing of pixels that do not count (whatever stands there).
 template <typename CoefT, bool VEC>
-__device__ __forceinline__ void keep_words(uint32_t (&keep)[4], const uint8_t* mask, int left, int lane)
+__device__ __forceinline__ void keep_words(uint32_t (&keep)[NW], const uint8_t* mask, int left, int lane)
 {
     using L = Lane<CoefT>;
+    constexpr int PX = NW * L::PER;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) keep[j] = L::kMagnitude;
+    for (int j = 0; j < NW; ++j) keep[j] = L::kMagnitude;
     if (mask) {
-        bool on[L::PX];
+        bool on[PX];
 #pragma unroll
-        for (int i = 0; i < L::PX; ++i) {
-            const int px = slot_pixel<L::PX, VEC>(lane, i);
+        for (int i = 0; i < PX; ++i) {
+            const int px = slot_pixel<PX, VEC>(lane, i);
             on[i] = px < left && __ldg(mask + px) != 0;
         }
 #pragma unroll
-        for (int j = 0; j < 4; ++j) keep[j] = L::keep(on, j);
+        for (int j = 0; j < NW; ++j) keep[j] = L::keep(on, j);
     }
 }
 
 template <int PX, bool VEC> __device__ __forceinline__ void put_pixels(float* row, const float (&v)[PX], int lane)
 {
-    if (VEC) {
+    if (VEC && PX % 4 == 0) {
 #pragma unroll
         for (int j = 0; j < PX / 4; ++j) *reinterpret_cast<float4*>(row + lane * PX + 4 * j) = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+    } else if (VEC) {
+#pragma unroll
+        for (int j = 0; j < PX / 2; ++j) *reinterpret_cast<float2*>(row + lane * PX + 2 * j) = make_float2(v[2 * j], v[2 * j + 1]);
     } else {
 #pragma unroll
         for (int i = 0; i < PX; ++i) row[lane + 32 * i] = v[i];
@@ -99,11 +115,17 @@ template <int PX, bool VEC> __device__ __forceinline__ void put_pixels(float* ro
 }
 template <int PX, bool VEC> __device__ __forceinline__ void get_pixels(float (&v)[PX], const float* row, int lane)
 {
-    if (VEC) {
+    if (VEC && PX % 4 == 0) {
 #pragma unroll
         for (int j = 0; j < PX / 4; ++j) {
             const float4 t = *reinterpret_cast<const float4*>(row + lane * PX + 4 * j);
             v[4 * j] = t.x; v[4 * j + 1] = t.y; v[4 * j + 2] = t.z; v[4 * j + 3] = t.w;
+        }
+    } else if (VEC) {
+#pragma unroll
+        for (int j = 0; j < PX / 2; ++j) {
+            const float2 t = *reinterpret_cast<const float2*>(row + lane * PX + 2 * j);
+            v[2 * j] = t.x; v[2 * j + 1] = t.y;
         }
     } else {
 #pragma unroll
@@ -123,13 +145,15 @@ struct BalanceParams {
     int64_t HW;
 };
 
-// (blocks a multiprocessor: as many as the registers of AW atoms allow)
+// Threads of a multiprocessor that leave each the registers for its words and what it does with them.
+constexpr int resident_threads(int words) { return words <= 24 ? 1024 : words <= 36 ? 768 : 512; }
+
 template <typename CoefT, int AW, int WARPS, bool VEC>
-__global__ void __launch_bounds__(WARPS * 32, (AW <= 9 ? 768 : 512) / (WARPS * 32))
+__global__ void __launch_bounds__(WARPS * 32, resident_threads(AW * NW) / (WARPS * 32))
 balance_kernel(const CoefT* __restrict__ coef, const __grid_constant__ BalanceParams p)
 {
     using L = Lane<CoefT>;
-    constexpr int PX = L::PX, TP = 32 * PX, NT = WARPS * 32, RANKS = NT / TP;   // threads a pixel
+    constexpr int PX = NW * L::PER, TP = 32 * PX, NT = WARPS * 32, RANKS = NT / TP;   // threads a pixel
     constexpr int COPIES = 8;                    // of the histogram: fewer threads of a warp meet on a counter
     __shared__ __align__(16) float ssum[WARPS][TP];
     __shared__ __align__(16) float sr[TP];
@@ -151,7 +175,7 @@ balance_kernel(const CoefT* __restrict__ coef, const __grid_constant__ BalancePa
     __syncthreads();
     for (int64_t p0 = (int64_t)b * TP; p0 < HW; p0 += (int64_t)p.bx * TP) {
         const int left = (int)min((int64_t)TP, HW - p0);
-        uint32_t x[AW][4], keep[4];
+        uint32_t x[AW][NW], keep[NW];
         load_words<CoefT, AW, WARPS, VEC>(x, frame + p0, HW, left, D, warp, lane);
         const bool on = px < left && (!frame_mask || __ldg(frame_mask + p0 + px) != 0);
         if (on) {                                // counts of the listed atoms
@@ -177,9 +201,9 @@ balance_kernel(const CoefT* __restrict__ coef, const __grid_constant__ BalancePa
 #pragma unroll
         for (int a = 0; a < AW; ++a) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) x[a][j] &= keep[j];
+            for (int j = 0; j < NW; ++j) x[a][j] &= keep[j];
 #pragma unroll
-            for (int i = 0; i < PX; ++i) sum[i] += L::get(x[a], i);
+            for (int i = 0; i < PX; ++i) sum[i] = L::add(x[a], i, sum[i]);
         }
         put_pixels<PX, VEC>(ssum[warp], sum, lane);
         __syncthreads();
@@ -237,45 +261,45 @@ struct BalanceSumParams {
     int n, D, s, bx, per_frame;
 };
 
-// Block (atoms 8 a .. 8 a + 7, frame f) adds up the frame's partial sums, 128 threads to an atom and a tree of fixed shape; the block
-// that finishes last then knows every frame's sums and writes slopes and loss.
-constexpr int kSumAtoms = 8;
-__global__ void __launch_bounds__(1024)
+// Block (frame f, atoms 8 a .. 8 a + 7) adds up the frame's partial sums: 32 threads to an atom, first within a warp, then over the
+// eight warps in order; the block that finishes last then knows every frame's sums and writes slopes and loss.
+constexpr int kSumAtoms = 8, kSumThreads = 256;
+__global__ void __launch_bounds__(kSumThreads)
 balance_sum_kernel(const __grid_constant__ BalanceSumParams p)
 {
-    __shared__ double ssum[1024];
-    __shared__ int scnt[1024];
-    __shared__ int svalid;
+    __shared__ double ssum[kSumThreads / 32][kSumAtoms];
+    __shared__ int scnt[kSumThreads / 32][kSumAtoms], svalid[kSumThreads / 32];
     __shared__ bool last;
-    const int tid = threadIdx.x, f = blockIdx.x, D = p.D, i8 = tid % kSumAtoms, g = tid / kSumAtoms, l = blockIdx.y * kSumAtoms + i8;
-    if (tid == 0) svalid = 0;
+    const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, f = blockIdx.x, D = p.D;
+    const int i8 = tid % kSumAtoms, g = tid / kSumAtoms, l = blockIdx.y * kSumAtoms + i8;
     wait_for_launch_before();
-    __syncthreads();
     double acc = 0.0;
     int c = 0, v = 0;
-#pragma unroll 4
-    for (int b = g; b < p.bx; b += 1024 / kSumAtoms) {
-        const int64_t row = (int64_t)f * p.bx + b;
-        if (l < D) {
-            acc += (double)__ldg(p.part_share + row * D + l);
-            c += __ldg(p.part_count + row * (D + 1) + l);
-        }
-        if (i8 == 0) v += __ldg(p.part_count + row * (D + 1) + D);
+    const float* ps = p.part_share + (int64_t)f * p.bx * D + min(l, D - 1);
+    const int32_t* pc = p.part_count + (int64_t)f * p.bx * (D + 1);
+#pragma unroll 8
+    for (int b = g; b < p.bx; b += kSumThreads / kSumAtoms) {
+        acc += (double)__ldg(ps + (int64_t)b * D);
+        c += __ldg(pc + (int64_t)b * (D + 1) + min(l, D - 1));
+        if (i8 == 0) v += __ldg(pc + (int64_t)b * (D + 1) + D);
+    }
+#pragma unroll
+    for (int o = 16; o >= kSumAtoms; o >>= 1) {
+        acc += __shfl_xor_sync(0xffffffffu, acc, o);
+        c += __shfl_xor_sync(0xffffffffu, c, o);
     }
     v = __reduce_add_sync(0xffffffffu, v);
-    if (tid % 32 == 0) atomicAdd(&svalid, v);
-    ssum[tid] = acc;
-    scnt[tid] = c;
-    for (int o = 512; o >= kSumAtoms; o >>= 1) {
-        __syncthreads();
-        if (tid < o) { ssum[tid] += ssum[tid + o]; scnt[tid] += scnt[tid + o]; }
-    }
+    if (lane < kSumAtoms) { ssum[warp][lane] = acc; scnt[warp][lane] = c; }
+    if (lane == 0) svalid[warp] = v;
     __syncthreads();
-    const int valid = svalid;
+    int valid = 0;
+#pragma unroll
+    for (int w = 0; w < kSumThreads / 32; ++w) valid += svalid[w];
     if (tid < kSumAtoms && l < D) {
-        p.share_sum[(int64_t)f * D + l] = ssum[tid];
-        p.counts[(int64_t)f * D + l] = scnt[tid];
-        p.share[(int64_t)f * D + l] = valid ? (float)(ssum[tid] / valid) : 0.f;
+        for (int w = 1; w < kSumThreads / 32; ++w) { acc += ssum[w][tid]; c += scnt[w][tid]; }
+        p.share_sum[(int64_t)f * D + l] = acc;
+        p.counts[(int64_t)f * D + l] = c;
+        p.share[(int64_t)f * D + l] = valid ? (float)(acc / valid) : 0.f;
     }
     if (tid == 0 && blockIdx.y == 0) p.valid[f] = valid;
     __threadfence();
@@ -287,7 +311,7 @@ balance_sum_kernel(const __grid_constant__ BalanceSumParams p)
     // counts of the batch by atom, or each frame's own
     double part = 0.0;
     if (p.per_frame) {
-        for (int64_t i = tid; i < (int64_t)p.n * D; i += 1024) {
+        for (int64_t i = tid; i < (int64_t)p.n * D; i += kSumThreads) {
             const double T = (double)__ldcg(p.valid + i / D);
             const double a = T > 0.0 ? (double)D * __ldcg(p.counts + i) / ((double)p.s * p.n * T * T) : 0.0;
             p.slope[i] = (float)a;
@@ -295,32 +319,29 @@ balance_sum_kernel(const __grid_constant__ BalanceSumParams p)
         }
     } else {
         __shared__ double count[256];
-        __shared__ double total;
-        if (tid == 0) {
-            double t = 0.0;
-            for (int i = 0; i < p.n; ++i) t += (double)__ldcg(p.valid + i);
-            total = t;
-        }
+        double T = 0.0;
+        for (int i = 0; i < p.n; ++i) T += (double)__ldcg(p.valid + i);
         if (tid < D) {
             double t = 0.0;
             for (int i = 0; i < p.n; ++i) t += (double)__ldcg(p.counts + (int64_t)i * D + tid);
-            count[tid] = t;
+            count[tid] = T > 0.0 ? (double)D * t / ((double)p.s * T * T) : 0.0;
         }
         __syncthreads();
-        const double T = total;
-        for (int64_t i = tid; i < (int64_t)p.n * D; i += 1024) {
-            const double a = T > 0.0 ? (double)D * count[i % D] / ((double)p.s * T * T) : 0.0;
+        for (int64_t i = tid; i < (int64_t)p.n * D; i += kSumThreads) {
+            const double a = count[i % D];
             p.slope[i] = (float)a;
             part += a * __ldcg(p.share_sum + i);
         }
     }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) part += __shfl_xor_sync(0xffffffffu, part, o);
     __syncthreads();
-    ssum[tid] = part;
-    for (int o = 512; o > 0; o >>= 1) {
-        __syncthreads();
-        if (tid < o) ssum[tid] += ssum[tid + o];
+    if (lane == 0) ssum[warp][0] = part;
+    __syncthreads();
+    if (tid == 0) {
+        for (int w = 1; w < kSumThreads / 32; ++w) part += ssum[w][0];
+        *p.loss = (float)part;
     }
-    if (tid == 0) *p.loss = (float)ssum[0];
 }
 
 // ---- backward --------------------------------------------------------------------------------------------------------------
@@ -334,7 +355,8 @@ struct BalanceGradParams {
     int64_t HW;
 };
 
-// Two results of a word: the factor of the magnitude with the coefficient's sign, zero where the coefficient is.
+// The results of a word: the factors d of the magnitudes with the coefficients' signs, zero where a coefficient is; or those added to
+// the word `old`. (A NaN in a pixel that does not count meets d = 0.)
 template <bool ADD> __device__ __forceinline__ uint32_t result_word(const float*, uint32_t x, uint32_t old, const float* d)
 {
     const float g = __uint_as_float(x) == 0.f ? 0.f : __uint_as_float(__float_as_uint(d[0]) ^ (x & 0x80000000u));
@@ -342,25 +364,27 @@ template <bool ADD> __device__ __forceinline__ uint32_t result_word(const float*
 }
 template <bool ADD> __device__ __forceinline__ uint32_t result_word(const __half*, uint32_t x, uint32_t old, const float* d)
 {
-    const __half2 h = *reinterpret_cast<const __half2*>(&x);
-    const uint32_t some = __hne2_mask(h, __half2half2(__ushort_as_half(0)));       // (NaN != 0)
+    const uint32_t some = __hne2_mask(*reinterpret_cast<const __half2*>(&x), __half2half2(__ushort_as_half(0)));
     if (!ADD) {                                  // rounding is symmetric: the sign may come after it
         const __half2 g = __floats2half2_rn(d[0], d[1]);
         return (*reinterpret_cast<const uint32_t*>(&g) ^ (x & 0x80008000u)) & some;
     }
-    const float g0 = (some & 1u) ? __uint_as_float(__float_as_uint(d[0]) ^ ((x & 0x8000u) << 16)) : 0.f;
-    const float g1 = (some >> 31) ? __uint_as_float(__float_as_uint(d[1]) ^ (x & 0x80000000u)) : 0.f;
-    const __half2 o = *reinterpret_cast<const __half2*>(&old);
-    const __half2 g = __floats2half2_rn(__low2float(o) + g0, __high2float(o) + g1);
+    const uint32_t sign = ((x & 0x80008000u) | 0x3C003C00u) & some;              // +1, -1 or 0 each
+    const __half2 sg = *reinterpret_cast<const __half2*>(&sign), o = *reinterpret_cast<const __half2*>(&old);
+    const __half2 g = __floats2half2_rn(fmaf(__low2float(sg), d[0], __low2float(o)), fmaf(__high2float(sg), d[1], __high2float(o)));
     return *reinterpret_cast<const uint32_t*>(&g);
 }
 
+// Atoms whose gradient to add to is in flight: all of a warp's where the registers allow (binary16, 1080p, D = 72: 201 us with four and
+// three blocks a multiprocessor, 160 with all nine and two; fp32: 317 with four and three blocks, 371 with nine and two).
+template <typename CoefT, int AW> __host__ __device__ constexpr int ahead_of() { return Lane<CoefT>::PER == 2 && AW <= 9 ? AW : 4; }
+
 template <typename CoefT, int AW, int WARPS, bool VEC, bool ADD>
-__global__ void __launch_bounds__(WARPS * 32, (AW <= 9 ? 768 : 512) / (WARPS * 32))
+__global__ void __launch_bounds__(WARPS * 32, resident_threads((AW + (ADD && VEC && ahead_of<CoefT, AW>() == AW ? AW : 0)) * NW) / (WARPS * 32))
 balance_grad_kernel(const CoefT* __restrict__ coef, CoefT* __restrict__ grad, const __grid_constant__ BalanceGradParams p)
 {
     using L = Lane<CoefT>;
-    constexpr int PX = L::PX, TP = 32 * PX, PER = PX / 4;        // elements of a word
+    constexpr int PER = L::PER, PX = NW * PER, TP = 32 * PX;
     __shared__ __align__(16) float ssum[WARPS][TP];
     __shared__ __align__(16) float sdot[WARPS][TP];
     __shared__ __align__(16) float sk[TP];                       // weight / S
@@ -372,7 +396,7 @@ balance_grad_kernel(const CoefT* __restrict__ coef, CoefT* __restrict__ grad, co
     const int64_t HW = p.HW;
     const int left = (int)min((int64_t)TP, HW - p0);
     const uint8_t* tile_mask = p.mask ? p.mask + (int64_t)f * HW + p0 : nullptr;
-    uint32_t x[AW][4], keep[4];
+    uint32_t x[AW][NW], keep[NW];
     load_words<CoefT, AW, WARPS, VEC>(x, coef + (int64_t)f * D * HW + p0, HW, left, D, warp, lane);
     keep_words<CoefT, VEC>(keep, tile_mask, left, lane);
     float a[AW];
@@ -383,15 +407,26 @@ balance_grad_kernel(const CoefT* __restrict__ coef, CoefT* __restrict__ grad, co
     for (int i = 0; i < PX; ++i) sum[i] = dot[i] = 0.f;
 #pragma unroll
     for (int j = 0; j < AW; ++j) {
-        uint32_t m[4];
+        uint32_t m[NW];
 #pragma unroll
-        for (int w = 0; w < 4; ++w) m[w] = x[j][w] & keep[w];
+        for (int w = 0; w < NW; ++w) m[w] = x[j][w] & keep[w];
 #pragma unroll
         for (int i = 0; i < PX; ++i) {
             const float v = L::get(m, i);
             sum[i] += v;
             dot[i] = fmaf(a[j], v, dot[i]);
         }
+    }
+    CoefT* dst = grad + ((int64_t)f * D + warp) * HW + p0 + (VEC ? lane * PX : lane);
+    // what is added to is asked for ahead (a load cannot pass the stores before it)
+    constexpr int AHEAD = ADD && VEC ? ahead_of<CoefT, AW>() : 1;
+    uint4 ahead[AHEAD];
+    auto ask = [&](int j) {
+        if (warp + j * WARPS < D && lane * PX < left) ahead[j % AHEAD] = *reinterpret_cast<const uint4*>(dst + (int64_t)j * WARPS * HW);
+    };
+    if (ADD && VEC) {
+#pragma unroll
+        for (int j = 0; j < (AHEAD < AW ? AHEAD : AW); ++j) ask(j);
     }
     put_pixels<PX, VEC>(ssum[warp], sum, lane);
     put_pixels<PX, VEC>(sdot[warp], dot, lane);
@@ -410,29 +445,36 @@ balance_grad_kernel(const CoefT* __restrict__ coef, CoefT* __restrict__ grad, co
     float k[PX], c[PX];
     get_pixels<PX, VEC>(k, sk, lane);
     get_pixels<PX, VEC>(c, sc, lane);
-    CoefT* dst = grad + ((int64_t)f * D + warp) * HW + p0 + (VEC ? lane * PX : lane);
+    bool all = true;                             // this warp's pixels all count
+    if (ADD) {
 #pragma unroll
-    for (int j = 0; j < AW; ++j, dst += WARPS * HW) {
+        for (int i = 0; i < PX; ++i) all &= k[i] != 0.f;
+        all = __all_sync(0xffffffffu, all);
+    }
+    auto finish = [&](auto every) {              // `every`: all pixels of the warp count
+#pragma unroll
+    for (int j = 0; j < AW; ++j) {
         if (warp + j * WARPS >= D) break;
-        uint32_t old[4] = {0u, 0u, 0u, 0u}, o[4];
+        CoefT* to = dst + (int64_t)j * WARPS * HW;
+        uint32_t old[NW], o[NW];
+#pragma unroll
+        for (int w = 0; w < NW; ++w) old[w] = 0u;
         if (ADD) {
             if (VEC) {
-                if (lane * PX < left) {
-                    const uint4 t = *reinterpret_cast<const uint4*>(dst);
-                    old[0] = t.x; old[1] = t.y; old[2] = t.z; old[3] = t.w;
-                }
+                unpack(old, ahead[j % AHEAD]);
+                if (j + AHEAD < AW) ask(j + AHEAD);
             } else {
 #pragma unroll
-                for (int i = 0; i < PX; ++i) L::put(old, i, lane + 32 * i < left ? L::one(dst + 32 * i) : 0u);
+                for (int i = 0; i < PX; ++i) L::put(old, i, lane + 32 * i < left ? L::one(to + 32 * i) : 0u);
             }
         }
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
+        for (int w = 0; w < NW; ++w) {
             float d[PER];
 #pragma unroll
             for (int i = 0; i < PER; ++i) d[i] = fmaf(a[j], k[w * PER + i], c[w * PER + i]);
             o[w] = result_word<ADD>((const CoefT*)nullptr, x[j][w], old[w], d);
-            if (ADD) {                           // a pixel that does not count keeps its bits
+            if (ADD && !decltype(every)::value) {                   // a pixel that does not count keeps its bits
 #pragma unroll
                 for (int i = 0; i < PER; ++i) {
                     const uint32_t part = PER == 1 ? 0xFFFFFFFFu : 0xFFFFu << (16 * i);
@@ -441,17 +483,20 @@ balance_grad_kernel(const CoefT* __restrict__ coef, CoefT* __restrict__ grad, co
             }
         }
         if (VEC) {
-            if (lane * PX < left) *reinterpret_cast<uint4*>(dst) = make_uint4(o[0], o[1], o[2], o[3]);
+            if (lane * PX < left) *reinterpret_cast<uint4*>(to) = make_uint4(o[0], o[1], o[2], o[3]);
         } else {
 #pragma unroll
             for (int i = 0; i < PX; ++i) {
                 if (lane + 32 * i < left) {
-                    if (PER == 1) dst[32 * i] = *reinterpret_cast<const CoefT*>(&o[i / PER]);
-                    else reinterpret_cast<unsigned short*>(dst)[32 * i] = (unsigned short)(i % 2 ? o[i / PER] >> 16 : o[i / PER] & 0xFFFFu);
+                    if (PER == 1) to[32 * i] = *reinterpret_cast<const CoefT*>(&o[i / PER]);
+                    else reinterpret_cast<unsigned short*>(to)[32 * i] = (unsigned short)(i % 2 ? o[i / PER] >> 16 : o[i / PER] & 0xFFFFu);
                 }
             }
         }
     }
+    };
+    if (!ADD || all) finish(std::true_type{});
+    else finish(std::false_type{});
 }
 
 // ---- host ------------------------------------------------------------------------------------------------------------------
@@ -505,9 +550,10 @@ cudaError_t backward_t(const BalanceArgs& a, const BalanceGradParams& p, void* g
     return cudaGetLastError();
 }
 
-// Atoms of a warp (registers) and warps of a block by D.
-#define SR_BALANCE_BY_ATOMS(D, call)                                   \
-    ((D) <= 16 ? call(2, 8) : (D) <= 32 ? call(4, 8) : (D) <= 48 ? call(6, 8) : (D) <= 72 ? call(9, 8) : (D) <= 80 ? call(10, 8) : (D) <= 128 ? call(8, 16) : call(16, 16))
+// Atoms of a warp and warps of a block by D.
+#define SR_BALANCE_BY_ATOMS(D, call)                                                                                                  \
+    ((D) <= 16 ? call(2, 8) : (D) <= 32 ? call(4, 8) : (D) <= 48 ? call(6, 8) : (D) <= 72 ? call(9, 8) : (D) <= 96 ? call(12, 8) \
+     : (D) <= 128 ? call(16, 8) : (D) <= 192 ? call(12, 16) : call(16, 16))
 
 template <typename CoefT> cudaError_t forward(const BalanceArgs& a, const BalanceParams& p, bool vec)
 {
@@ -546,7 +592,7 @@ cudaError_t launch_balance(const BalanceArgs& a)
     if (cudaError_t e = a.coef_dtype == SR_F16 ? forward<__half>(a, p, vec) : forward<float>(a, p, vec)) return e;
     const BalanceSumParams q{sc.part_share, sc.part_count, sc.ticket, sc.share_sum, sc.valid, a.counts, a.share, a.slope, a.loss,
                              a.n, a.D, a.s, bx, a.per_frame ? 1 : 0};
-    if (cudaError_t e = launch_after(balance_sum_kernel, dim3(a.n, (a.D + kSumAtoms - 1) / kSumAtoms), 1024, a.st, q)) return e;
+    if (cudaError_t e = launch_after(balance_sum_kernel, dim3(a.n, (a.D + kSumAtoms - 1) / kSumAtoms), kSumThreads, a.st, q)) return e;
     count_launches(2);
     return cudaSuccess;
 }
