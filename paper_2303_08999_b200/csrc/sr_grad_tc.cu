@@ -54,6 +54,7 @@ struct GradTcParams {
     int rows;                    // planes of the product: D, or s of a compact subset (first product); D, or s of a subset (second)
     int planes;                  // planes of a frame in coef / gcoef
     int stage_bytes, chunk_bytes;
+    int own_out;                 // first product: bytes of a group's buffer for results; 0 = they pass through the G tile
     int tma;                     // second product: coefficients arrive by TMA
     long long wait_cycles;
     int lose;                    // test hook: the first commit of block 0 is left out
@@ -86,6 +87,34 @@ __device__ __forceinline__ void tma_store_4d(const CUtensorMap* map, const void*
 __device__ __forceinline__ void bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
 __device__ __forceinline__ void bulk_wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
 __device__ __forceinline__ void bulk_wait_all() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+// Waits of a row's length (some hundred cycles): tested without the time hint of mbar_wait, whose sleep is longer than they are
+// (1080p x4, D = 72, k = 5: coefficients 137 -> 104 us, dictionary 129 -> 98). Bounded like it.
+__device__ __forceinline__ bool mbar_wait_short(uint64_t* bar, uint32_t parity, volatile WaitCtx* wc)
+{
+    const uint32_t at = smem_u32(bar);
+    const long long t0 = clock64();
+    while (true) {
+#pragma unroll 1
+        for (int i = 0; i < 32; ++i) {
+            uint32_t done;
+            asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                         : "=r"(done) : "r"(at), "r"(parity) : "memory");
+            if (done) return true;
+        }
+        if (wc->abort_flag) return false;
+        if (clock64() - t0 > const_cast<const WaitCtx*>(wc)->limit) {
+            wc->abort_flag = 1;
+            return false;
+        }
+    }
+}
+// One lane of a converged warp, known to the compiler as such (operands of what it issues stay in uniform registers).
+__device__ __forceinline__ bool elect_one()
+{
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
+    return r != 0;
+}
 __device__ __forceinline__ void cp_async_wait_all_() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 
 __device__ __forceinline__ unsigned finite_bits(float v) { const unsigned b = __float_as_uint(v) & 0x7FFFFFFFu; return b < 0x7F800000u ? b : 0u; }
@@ -201,19 +230,33 @@ template <int K> struct TileState {
     }
 };
 
-// G of a pixel, times the tile's scale.
-template <int K> __device__ __forceinline__ void patch_grad(const float* u, int u_channel, const float* g, int C, float scale, float (&G)[K * K])
+// G of a pixel, times the tile's scale. `between` is called after the first channel. One and three channels are written out: a loop
+// over channels carries its k*k sums from register to register (293 instructions a row and warp for three, 5 x 5; 165 written out).
+template <int K, int NC, typename Between>
+__device__ __forceinline__ void patch_grad_c(const float* u, int u_channel, const float* g, int C, float scale, float (&G)[K * K], Between between)
 {
     constexpr int UW = GGeo<K>::UW;
 #pragma unroll
-    for (int j = 0; j < K * K; ++j) G[j] = 0.f;
-    for (int c = 0; c < C; ++c, u += u_channel) {
-        const float gv = g[c * kGroupThreads] * scale;
+    for (int c = 0; c < NC; ++c) {
+        if (c < C) {
+            const float gv = g[c * kGroupThreads] * scale;
 #pragma unroll
-        for (int a = 0; a < K; ++a)
+            for (int a = 0; a < K; ++a)
 #pragma unroll
-            for (int b = 0; b < K; ++b) G[a * K + b] = fmaf(gv, u[a * UW + b], G[a * K + b]);
+                for (int b = 0; b < K; ++b) {
+                    const float v = u[c * u_channel + a * UW + b];
+                    G[a * K + b] = c == 0 ? gv * v : fmaf(gv, v, G[a * K + b]);
+                }
+        }
+        if (c == 0) between();
     }
+}
+template <int K, typename Between>
+__device__ __forceinline__ void patch_grad(const float* u, int u_channel, const float* g, int C, float scale, float (&G)[K * K], Between between)
+{
+    if (C == 3) patch_grad_c<K, 3>(u, u_channel, g, 3, scale, G, between);
+    else if (C == 1) patch_grad_c<K, 1>(u, u_channel, g, 1, scale, G, between);
+    else patch_grad_c<K, kMaxC>(u, u_channel, g, C, scale, G, between);
 }
 
 __device__ __forceinline__ void init_ctl(GradCtl& ctl, const GradTcParams& p, int tid)
@@ -245,7 +288,7 @@ __device__ __forceinline__ Floats carve_floats(uint8_t* at, const GradTcParams& 
 
 // The first product in one of two layouts of its result.
 //   ATOMS: accumulator lane = atom, column = pixel (atoms are the rows of the product). A warp puts its 32 atoms' values of 64 pixels
-//          into 4 KB of shared memory (its part of the G tile, which the product has read by then, where the atoms are at most 128) and one TMA store takes them to
+//          into 4 KB of shared memory (a buffer of its own, or its part of the G tile, which the product has read by then) and one TMA store takes them to
 //          their planes; needs W % 8 == 0. Storing a lane's row directly, 32 bytes at a time, touches 32 planes an instruction: 268 us
 //          at 1080p x4, D = 72, where one value of one plane per instruction (below) takes 223.
 //   else:  lane = pixel, column = atom. A thread stores its pixel's value of one plane after the other, 64 bytes a warp, whatever the
@@ -260,14 +303,15 @@ grad_coef_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_consta
     __shared__ float sback[256];                 // 2^e of each plane's atom (0: a plane outside the subset)
     uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     const Problem& pb = p.g.pb;
-    const int tid = threadIdx.x, grp = tid / kGroupThreads, x = tid % kGroupThreads, lane = tid & 31, warp = tid >> 5;
+    const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), grp = warp / (kGroupThreads / 32), x = tid % kGroupThreads, lane = tid & 31;
+    const bool leads = warp % (kGroupThreads / 32) == 0;         // the group's first warp: its elected lane issues what one thread issues
     const int C = pb.c, D = pb.D, W = pb.W, rows_pad = (p.rows + 15) & ~15;
     uint8_t* sG = smem + grp * G::G_BYTES;
     uint8_t* sD = smem + kGroups * G::G_BYTES;   // [column][rows_pad][128 B]
     const int d_block = rows_pad * 128;
-    // results on their way out: in the G tile, or, where a second product of the same row still reads that, behind the atoms
-    uint8_t* sOut = ATOMS && p.rows > 128 ? sD + G::BLOCKS * d_block + grp * kOutBytes : sG;
-    const Floats s = carve_floats(sD + G::BLOCKS * d_block + (ATOMS && p.rows > 128 ? kGroups * kOutBytes : 0), p, G::UW);
+    // results on their way out: behind the atoms (4 KB for each warp that has some), or in the G tile
+    uint8_t* sOut = ATOMS && p.own_out ? sD + G::BLOCKS * d_block + grp * p.own_out : sG;
+    const Floats s = carve_floats(sD + G::BLOCKS * d_block + (ATOMS ? kGroups * p.own_out : 0), p, G::UW);
 
     init_ctl(ctl, p, tid);
     for (int i = tid; i < (kGroups * G::G_BYTES + G::BLOCKS * d_block) / 16; i += kThreads) reinterpret_cast<uint4*>(smem)[i] = make_uint4(0, 0, 0, 0);
@@ -312,7 +356,7 @@ grad_coef_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_consta
     const uint64_t d_desc = make_smem_desc(smem_u32(sD), 16, 1024, kSwizzle128B);
     constexpr uint32_t kGLo = (G::BLOCKS == 2 ? 128 * 128 : G::LO_CHUNK * 16) >> 4;
     const uint32_t kDLo = (uint32_t)(G::BLOCKS == 2 ? d_block : G::LO_CHUNK * 16) >> 4;
-    bool lose = p.lose != 0 && blockIdx.x == 0 && tid == 0;
+    bool lose = p.lose != 0 && blockIdx.x == 0 && warp == 0;
     uint32_t phase = 0;
     bool ok = true;
     int parity = 0;
@@ -320,42 +364,37 @@ grad_coef_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_consta
         const LrWindow w = ts.w;
         if (!(ok = ts.make(p, ctl, t, parity, s.L, s.V, s.U, s.g, tid, ok))) break;
         const bool inside = w.x0 + x < W;
-        for (int row = grp; row < w.rows; row += kGroups) {
-            float v[G::kk];
-            patch_grad<K>(s.U + row * G::UW + x, p.g.uh * G::UW, s.g + row * C * kGroupThreads + x, C, ts.scale, v);
-            if (ATOMS) {                         // every warp's stores have read the tile
-                if (lane == 0) bulk_wait_read();
-                ok = group_barrier_and(1 + grp, ok);
+        const uint32_t at = tmem + ((uint32_t)(32 * (warp & 3)) << 16);
+        auto multiply = [&](int m0) {            // thread 0 of the group: planes m0 .. m0 + 127 of the row in sG
+            tc_fence_after_sync();
+            const int nr = min(128, p.rows - m0);
+            const uint32_t idesc = make_idesc_f16(128, ATOMS ? 128 : (nr + 15) & ~15, false, false);
+            const uint64_t dd = d_desc + (uint64_t)((uint32_t)m0 * 128u >> 4);
+#pragma unroll
+            for (int ks = 0; ks < G::KSTEPS; ++ks) {
+                const uint64_t gh = g_desc + 2 * ks, gl = gh + kGLo, dh = dd + 2 * ks, dl = dh + kDLo;
+                mma_f16_ss(tmem, ATOMS ? dh : gh, ATOMS ? gh : dh, idesc, ks > 0);
+                mma_f16_ss(tmem, ATOMS ? dh : gl, ATOMS ? gl : dh, idesc, 1u);
+                mma_f16_ss(tmem, ATOMS ? dl : gh, ATOMS ? gh : dl, idesc, 1u);
             }
-            write_row<K>(sG, 128 * 128, x, v);
+            if (!lose) mma_commit(&ctl.mma[grp]);
+            lose = false;
+        };
+        // The results of a row whose product has been started. False: the group leaves (all of it).
+        auto finish = [&](int row) {
             const int64_t pix = (int64_t)(w.y0 + row) * W + w.x0 + x;
-            bool go = true;                      // the group's: a thread leaves only where all do
             for (int m0 = 0; m0 < p.rows; m0 += 128) {
                 const int nr = min(128, p.rows - m0);
-                fence_proxy_async_smem();
-                tc_fence_before_sync();
-                go = group_barrier_and(1 + grp, ok);
-                if (!go) break;
-                if (x == 0) {
-                    tc_fence_after_sync();
-                    const uint32_t idesc = make_idesc_f16(128, ATOMS ? 128 : (nr + 15) & ~15, false, false);
-                    const uint64_t dd = d_desc + (uint64_t)((uint32_t)m0 * 128u >> 4);
-#pragma unroll
-                    for (int ks = 0; ks < G::KSTEPS; ++ks) {
-                        const uint64_t gh = g_desc + 2 * ks, gl = gh + kGLo, dh = dd + 2 * ks, dl = dh + kDLo;
-                        mma_f16_ss(tmem, ATOMS ? dh : gh, ATOMS ? gh : dh, idesc, ks > 0);
-                        mma_f16_ss(tmem, ATOMS ? dh : gl, ATOMS ? gl : dh, idesc, 1u);
-                        mma_f16_ss(tmem, ATOMS ? dl : gh, ATOMS ? gh : dl, idesc, 1u);
-                    }
-                    if (lose) lose = false;
-                    else mma_commit(&ctl.mma[grp]);
+                if (m0 > 0) {
+                    tc_fence_before_sync();
+                    if (!group_barrier_and(1 + grp, ok)) return false;
+                    if (leads && elect_one()) multiply(m0);
+                    __syncwarp();
                 }
-                __syncwarp();
-                ok = __all_sync(0xffffffffu, mbar_wait(&ctl.mma[grp], phase, wc));
+                ok = __all_sync(0xffffffffu, ok && mbar_wait_short(&ctl.mma[grp], phase, wc));
                 phase ^= 1;
                 tc_fence_after_sync();
                 if (!ok) continue;               // (the next barrier tells the group)
-                const uint32_t at = tmem + ((uint32_t)(32 * (warp & 3)) << 16);
                 if (ATOMS) {
                     const int l = 32 * (warp & 3) + lane;
                     if (l - lane < nr) {
@@ -373,13 +412,15 @@ grad_coef_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_consta
 #pragma unroll
                                 for (int i = 0; i < 16; ++i) {
                                     const __half2 v2 = __floats2half2_rn(acc[2 * i] * k, acc[2 * i + 1] * k);
-                                    h[c1 / 2 + i] = back != 0.f ? *reinterpret_cast<const uint32_t*>(&v2) : 0u;
+                                    h[c1 / 2 + i] = *reinterpret_cast<const uint32_t*>(&v2);
                                 }
                             }
-                            if (c0 > 0 || m0 > 0) {                          // the store before has read the buffer
-                                if (lane == 0) bulk_wait_read();
-                                __syncwarp();
+                            if (back == 0.f) {               // outside the subset: zeros, whatever G is
+#pragma unroll
+                                for (int i = 0; i < 32; ++i) h[i] = 0u;
                             }
+                            if (lane == 0) bulk_wait_read(); // the store before has read the buffer
+                            __syncwarp();
 #pragma unroll
                             for (int j = 0; j < 8; ++j)
                                 *reinterpret_cast<uint4*>(mine + lane * 128 + ((j ^ (lane & 7)) << 4)) = make_uint4(h[4 * j], h[4 * j + 1], h[4 * j + 2], h[4 * j + 3]);
@@ -410,12 +451,34 @@ grad_coef_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_consta
                     }
                 }
             }
-            if (!go) { ok = false; break; }
+            return true;
+        };
+        bool go = true;                          // the group's: a thread leaves only where all do
+        int started = -1;                        // row whose product is under way while the next row's G is computed
+        for (int row = grp; row < w.rows; row += kGroups) {
+            float v[G::kk];
+            patch_grad<K>(s.U + row * G::UW + x, p.g.uh * G::UW, s.g + row * C * kGroupThreads + x, C, ts.scale, v, [] {});
+            if (started >= 0 && !(go = finish(started))) break;
+            if (ATOMS && !p.own_out) {           // every warp's stores have read the tile
+                if (lane == 0) bulk_wait_read();
+                ok = group_barrier_and(1 + grp, ok);
+            }
+            write_row<K>(sG, 128 * 128, x, v);
+            fence_proxy_async_smem();
+            tc_fence_before_sync();
+            if (!(go = group_barrier_and(1 + grp, ok))) break;
+            if (leads && elect_one()) multiply(0);
+            __syncwarp();
+            started = row;
         }
+        if (go && started >= 0) go = finish(started);
+        ok = ok && go;
+        tc_fence_before_sync();
     }
     // ---- teardown: every product finished before tensor memory is freed, every store before shared memory is
     if (ATOMS && lane == 0) bulk_wait_all();
-    if (x == 0) { mma_commit(&ctl.drain); mbar_wait_drain(&ctl.drain, 0); }
+    __syncwarp();
+    if (leads && elect_one()) { mma_commit(&ctl.drain); mbar_wait_drain(&ctl.drain, 0); }        // (the lane that issued them)
     __syncwarp();
     cp_async_wait_all_();
     tc_fence_before_sync();
@@ -439,7 +502,8 @@ grad_dict_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_consta
     __shared__ GradCtl ctl;
     uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     const Problem& pb = p.g.pb;
-    const int tid = threadIdx.x, grp = tid / kGroupThreads, x = tid % kGroupThreads, lane = tid & 31, warp = tid >> 5;
+    const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), grp = warp / (kGroupThreads / 32), x = tid % kGroupThreads, lane = tid & 31;
+    const bool leads = warp % (kGroupThreads / 32) == 0;         // the group's first warp: its elected lane issues what one thread issues
     const int C = pb.c, D = pb.D, W = pb.W, s_ = pb.s;
     uint8_t* sG = smem + grp * G::G_BYTES;
     uint8_t* sPhi = smem + kGroups * G::G_BYTES + grp * p.stage_bytes;         // [64-pixel chunk][plane][128 B]
@@ -470,10 +534,10 @@ grad_dict_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_consta
 #pragma unroll
         for (int j = 0; j < G::kk; ++j) total[m][j] = 0.f;
 
-    bool lose = p.lose != 0 && blockIdx.x == 0 && tid == 0;
+    bool lose = p.lose != 0 && blockIdx.x == 0 && warp == 0;
     uint32_t phase = 0, fphase = 0;
     bool in_work = false;                        // a product of this group whose end has not been waited for
-    bool landing = false;                        // (thread 0 of the group) a copy that has not been waited for
+    bool landing = false;                        // (the group's first warp) a copy that has not been waited for
     bool ok = true;
     int parity = 0;
     uint8_t* chunk = sPhi + (x >> 6) * p.chunk_bytes;
@@ -481,25 +545,33 @@ grad_dict_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_consta
     auto place = [&](int l) { return reinterpret_cast<__half*>(chunk + l * 128 + ((unit ^ (l & 7)) << 4) + at2); };
     for (int t = blockIdx.x; t < p.g.num_tiles; t += gridDim.x, parity ^= 1) {
         const LrWindow w = ts.w;
-        auto fetch = [&](int row) {              // thread 0 of the group: two boxes, bytes counted on full
+        auto fetch = [&](int row) {              // the group's first warp: two boxes, bytes counted on full
+            landing = true;
+            if (!elect_one()) return;
             mbar_arrive_expect_tx(&ctl.full[grp], (uint32_t)p.rows * 256u);
             tma_load_4d(sPhi, &map, &ctl.full[grp], w.x0, w.y0 + row, 0, w.f);
             tma_load_4d(sPhi + p.chunk_bytes, &map, &ctl.full[grp], w.x0 + 64, w.y0 + row, 0, w.f);
-            landing = true;
         };
-        if (p.tma && x == 0 && grp < w.rows && ok) fetch(grp);                  // (the tile before was waited for at its end)
+        if (p.tma && leads && grp < w.rows && ok) fetch(grp);                  // (the tile before was waited for at its end)
         __syncwarp();
         if (!(ok = ts.make(p, ctl, t, parity, s.L, s.V, s.U, s.g, tid, ok))) break;
         const bool inside = w.x0 + x < W;
         for (int row = grp; row < w.rows; row += kGroups) {
             float v[G::kk];
-            patch_grad<K>(s.U + row * G::UW + x, p.g.uh * G::UW, s.g + row * C * kGroupThreads + x, C, ts.scale, v);
+            patch_grad<K>(s.U + row * G::UW + x, p.g.uh * G::UW, s.g + row * C * kGroupThreads + x, C, ts.scale, v, [&] {
+                // by now the row before has been multiplied: its stage takes this row's coefficients while G is being computed
+                if (p.tma && in_work) {
+                    if (leads) {
+                        ok = __all_sync(0xffffffffu, ok && mbar_wait_short(&ctl.mma[grp], phase, wc));
+                        if (ok) fetch(row);
+                    }
+                    __syncwarp();
+                }
+            });
             if (in_work) {
-                ok = __all_sync(0xffffffffu, mbar_wait(&ctl.mma[grp], phase, wc));
+                ok = __all_sync(0xffffffffu, ok && mbar_wait_short(&ctl.mma[grp], phase, wc));
                 phase ^= 1;
                 in_work = false;
-                if (p.tma && x == 0 && ok) fetch(row);
-                __syncwarp();
             }
             if (!inside) {
 #pragma unroll
@@ -532,28 +604,29 @@ grad_dict_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_consta
             fence_proxy_async_smem();
             tc_fence_before_sync();
             if (!(ok = group_barrier_and(1 + grp, ok))) break;
-            if (x == 0) {
+            if (leads) {
                 bool there = true;
-                if (p.tma) { there = mbar_wait(&ctl.full[grp], fphase, wc); landing = !there; }
-                if (there) {
+                if (p.tma) { there = __all_sync(0xffffffffu, mbar_wait_short(&ctl.full[grp], fphase, wc)); landing = !there; }
+                if (there && elect_one()) {
                     tc_fence_after_sync();
 #pragma unroll
                     for (int m = 0; m < MB; ++m) {
+#pragma unroll
                         for (int ks = 0; ks < 8; ++ks) {
                             const uint64_t ad = a_desc + (uint64_t)((uint32_t)(m * 128 * 128 + (ks >> 2) * p.chunk_bytes + (ks & 3) * 32) >> 4);
                             mma_f16_ss(tmem + m * G::NB, ad, g_desc + (uint64_t)(ks * 2048 >> 4), idesc, row > grp || ks > 0);
                         }
                     }
-                    if (lose) lose = false;
-                    else mma_commit(&ctl.mma[grp]);
+                    if (!lose) mma_commit(&ctl.mma[grp]);
                 }
+                lose = false;
             }
             fphase ^= 1;
             in_work = true;
             __syncwarp();
             if (p.mode == kModeIdx || p.mode == kModeCompact) {
                 // the stage goes back to zeros, which needs the product's end
-                ok = __all_sync(0xffffffffu, mbar_wait(&ctl.mma[grp], phase, wc));
+                ok = __all_sync(0xffffffffu, mbar_wait_short(&ctl.mma[grp], phase, wc));
                 phase ^= 1;
                 in_work = false;
                 if (inside && ok)
@@ -564,7 +637,7 @@ grad_dict_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_consta
         if (!ok) continue;                       // (the next tile's barrier, or the end, tells the block)
         if (grp < w.rows) {
             if (in_work) {
-                ok = __all_sync(0xffffffffu, mbar_wait(&ctl.mma[grp], phase, wc));
+                ok = __all_sync(0xffffffffu, mbar_wait_short(&ctl.mma[grp], phase, wc));
                 phase ^= 1;
                 in_work = false;
             }
@@ -590,7 +663,8 @@ grad_dict_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_consta
         }
     }
     // ---- teardown
-    if (x == 0) {
+    __syncwarp();
+    if (leads && elect_one()) {                  // (the lane that issued copies and products)
         if (landing) mbar_wait_drain(&ctl.full[grp], fphase);
         mma_commit(&ctl.drain);
         mbar_wait_drain(&ctl.drain, 0);
@@ -699,12 +773,16 @@ bool encode_planes(CUtensorMap* map, const void* base, const Problem& pb, int pl
 // Plane rows that TMA can store.
 bool coef_atoms(const GradArgs& a) { return a.pb.W % 8 == 0 && ((uintptr_t)a.gcoef & 15) == 0 && encode_fn(); }
 
-template <int K> size_t coef_smem(Geom& g, const GradArgs& a)
+// own_out: bytes of a group's buffer for results. More than 128 atoms need one (the next product of the row reads G still); others
+// have one where two blocks fit a multiprocessor with it.
+template <int K> size_t coef_smem(Geom& g, const GradArgs& a, int* own_out)
 {
     const int rows_pad = (coef_rows(a) + 15) & ~15;
     const size_t before = 1024 + kGroups * GGeo<K>::G_BYTES;
-    const size_t all = before + (size_t)GGeo<K>::BLOCKS * rows_pad * 128 + (rows_pad > 128 && coef_atoms(a) ? kGroups * kOutBytes : 0) +
-                       float_bytes<K>(g, a.pb, a.lr);
+    const size_t rest = before + (size_t)GGeo<K>::BLOCKS * rows_pad * 128 + float_bytes<K>(g, a.pb, a.lr);
+    const int buffer = (rows_pad < 128 ? (rows_pad + 31) / 32 : 4) * (kOutBytes / 4);
+    *own_out = coef_atoms(a) && (rows_pad > 128 || blocks_per_sm(rest + kGroups * buffer) == 2) ? buffer : 0;
+    const size_t all = rest + kGroups * *own_out;
     // atoms as rows: the product reads them 128 at a time, whatever lies behind the last one must be shared memory
     const size_t reach = before + (size_t)(GGeo<K>::BLOCKS - 1) * rows_pad * 128 + (size_t)((rows_pad + 127) / 128) * 128 * 128;
     return all > reach ? all : reach;
@@ -742,7 +820,7 @@ template <int K, bool ATOMS> cudaError_t launch_coef_ka(const GradArgs& a)
 {
     GradTcParams p = common_params(a);
     if (!p.status) return cudaErrorUnknown;
-    const size_t smem = coef_smem<K>(p.g, a);
+    const size_t smem = coef_smem<K>(p.g, a, &p.own_out);
     p.rows = coef_rows(a);
     CUtensorMap map{};
     if (ATOMS && !encode_planes(&map, a.gcoef, a.pb, p.planes, 32)) return cudaErrorUnknown;
@@ -798,10 +876,11 @@ bool grad_coef_tc_supported(const GradArgs& a)
 {
     if (!form_supported(a) || a.mode == kModeIdx || a.mode == kModeCompact) return false;
     Geom g;
+    int own_out;
     switch (a.pb.k) {
-    case 3: return fits(coef_smem<3>(g, a));
-    case 5: return fits(coef_smem<5>(g, a));
-    default: return fits(coef_smem<7>(g, a));
+    case 3: return fits(coef_smem<3>(g, a, &own_out));
+    case 5: return fits(coef_smem<5>(g, a, &own_out));
+    default: return fits(coef_smem<7>(g, a, &own_out));
     }
 }
 
