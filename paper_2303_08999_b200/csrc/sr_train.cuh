@@ -41,6 +41,9 @@ bool grad_coef_tc_supported(const GradArgs& a);
 bool grad_dict_tc_supported(const GradArgs& a);
 cudaError_t launch_grad_coef_tc(const GradArgs& a);
 cudaError_t launch_grad_dict_tc(const GradArgs& a, int* slots);       // partial sums only
+// Both in one kernel of specialised warps, up to 128 atoms (sr_grad_roles.cu).
+bool grad_roles_supported(const GradArgs& a);
+cudaError_t launch_grad_roles(const GradArgs& a, int* slots);         // gcoef, and partial sums
 // Sums the partial sums of `slots` blocks into gdict and ggamma.
 cudaError_t launch_grad_dict_sum(const GradArgs& a, int slots);
 

@@ -11,9 +11,15 @@ bool on(const void* p, size_t a) { return ((uintptr_t)p % a) == 0; }
 
 cudaError_t run_grad(const GradArgs& a)
 {
+    const bool sums = a.gdict || a.ggamma;
+    if (grad_roles_supported(a)) {
+        int slots = 0;
+        if (cudaError_t e = launch_grad_roles(a, &slots)) return e;
+        return sums ? launch_grad_dict_sum(a, slots) : cudaSuccess;
+    }
     if (a.gcoef)
         if (cudaError_t e = grad_coef_tc_supported(a) ? launch_grad_coef_tc(a) : launch_grad_coef_fma(a)) return e;
-    if (a.gdict || a.ggamma) {
+    if (sums) {
         int slots = 0;
         if (cudaError_t e = grad_dict_tc_supported(a) ? launch_grad_dict_tc(a, &slots) : launch_grad_dict_fma(a, &slots)) return e;
         return launch_grad_dict_sum(a, slots);
