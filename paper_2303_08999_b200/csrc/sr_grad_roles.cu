@@ -5,13 +5,13 @@
 // (1080p x4, D = 72, k = 5: 129 + 129 us in two kernels, 34 of each the up-sampled tile, against 95 us of traffic). Here one block per
 // multiprocessor holds a pipeline, and G, which costs most, is computed once for both products:
 //   G warps (kFG groups of four)   the up-sampled tile; G of every row, hi + lo, into a ring of tiles         g_full
-//   load warps (three)             the row's coefficients into a ring of stages: TMA boxes, or (widths and    p_full
+//   load warps (two)               the row's coefficients into a ring of stages: TMA boxes, or (widths and    p_full
 //                                  addresses TMA does not take, gathered planes, lists) a pixel a thread
-//   MMA warp                       both products of a row; a row's filters in one of two accumulators         c_full, g_empty, p_empty
-//                                  (lane = atom, column = pixel), the dictionary's sums over the tile in      d_full
-//                                  one of two more
-//   result warps (four)            a row's coefficient gradients to memory (c_empty), the tile's dictionary sums to registers (d_empty)
+//   MMA warps (one a product)      a row's coefficient gradients in one of two accumulators (lane = atom,     c_full, g_empty
+//                                  column = pixel), the dictionary's sums over the tile in one of two more     d_full, p_empty, g_empty
+//   result warps (kRG groups of four)  a row's coefficient gradients to memory (c_empty), the tile's dictionary sums to registers (d_empty)
 // Rows are numbered through the block's tiles; row i goes to G group i mod kFG, ring entries i mod their count, accumulator i mod 2.
+// Waits suspend (mbar_wait): warps with time to spare must not take issue slots from those that set the pace.
 // Every wait is bounded: on expiry a warp raises the block's flag and leaves its loop, as every other does at its next wait.
 #include "sr_grad_tc.cuh"
 
@@ -24,12 +24,21 @@ using namespace tile;
 using namespace gradtc;
 
 constexpr int kFG = 2;                                       // groups of G warps
-// Sixteen warps, so that each has 128 registers; the result warps start at a multiple of four (their share of tensor memory).
-constexpr int kResultWarp = kFG * 4, kLoadWarp = kResultWarp + 4, kMmaWarp = kLoadWarp + 3;
-constexpr int kRoleThreads = (kMmaWarp + 1) * 32, kLoadThreads = 96;
-static_assert(kRoleThreads == 512, "128 registers a thread");
+constexpr int kRG = 2;                                       // groups of result warps: rows of one accumulator each
+constexpr int kResultWarp = kFG * 4, kLoadWarp = kResultWarp + kRG * 4, kMmaWarp = kLoadWarp + 2;
+constexpr int kRoleThreads = (kMmaWarp + 2) * 32, kLoadThreads = 64;
+// Registers a thread: of the launch, and after the G warps have taken what the others do not need (whole warpgroups; an increase beyond
+// what the block was launched with would wait for ever).
+constexpr int kRegsLaunch = 96, kRegsG = 112, kRegsResult = 104, kRegsLoad = 48;
+static_assert(kRegsG >= kRegsLaunch && kRegsResult >= kRegsLaunch && kRegsLoad <= kRegsLaunch, "inc, inc and dec below (the other direction is an illegal instruction)");
+static_assert(kRegsLaunch * kRoleThreads <= 65536, "the launch's registers fit the multiprocessor");
+static_assert(kFG * 128 * kRegsG + kRG * 128 * kRegsResult + 128 * kRegsLoad <= kRegsLaunch * kRoleThreads, "the roles' registers are the launch's");
+constexpr int kRoleReserve = 6656;                           // static shared memory, kept out of the dynamic budget
 constexpr int kMaxG = 4, kMaxP = 4, kUnscales = 16;
-template <int K> constexpr int kRing = K == 7 ? 2 : kMaxG;      // G tiles (those of 7 x 7 are twice as large)
+// G tiles (those of 7 x 7 are twice as large). At least as many as groups: a group that waits for a tile's use u must know that use u - 2
+// is over (a barrier tells only the parity of its phase); its own row before, kFG rows back, waited for the row kRing before that one.
+template <int K> constexpr int kRing = K == 7 ? 2 : kMaxG;
+static_assert(kRing<7> >= kFG && kRing<5> >= kFG, "a group is never two uses ahead of a ring entry");
 
 struct __align__(16) RoleCtl {
     GradCtl c;                                               // (its mma / full barriers are not used)
@@ -37,15 +46,17 @@ struct __align__(16) RoleCtl {
     uint64_t c_full[2], c_empty[2], d_full[2], d_empty[2];
     float unscale[kUnscales];                                // of the tiles, by number
     float back[128];                                         // 2^e of each plane's atom (0: a plane outside the subset)
-    uint32_t listed[128][4];                                 // lists: the row's pixels that list the atom
+    uint32_t listed[kRG][128][4];                            // lists: the pixels of a group's row that list the atom
 };
 
 struct RoleParams {
     GradTcParams b;
     int atoms;                   // rows of the first product: D, or s of a compact subset
+    int d_block;                 // bytes of a column of them
     int planes_in, planes_out;   // of a frame in coef and gcoef
     int p_stages;
     int tma_in, tma_out;
+    int copy_bytes;              // coefficients by asynchronous copies of this size; 0 = TMA or one by one
     int want_coef, want_dict;
 };
 
@@ -59,15 +70,15 @@ template <int K> __device__ __forceinline__ RoleSmem<K> carve(uint8_t* at, const
     RoleSmem<K> s;
     s.G = at;
     s.D = s.G + kRing<K> * GGeo<K>::G_BYTES;
-    s.out = s.D + (p.want_coef ? GGeo<K>::BLOCKS * 128 * 128 : 0);
-    s.Phi = s.out + (p.want_coef ? 2 * kOutBytes : 0);
+    s.out = s.D + (p.want_coef ? GGeo<K>::BLOCKS * p.d_block : 0);
+    s.Phi = s.out + (p.want_coef ? kRG * kOutBytes : 0);
     s.f = carve_floats(s.Phi + p.p_stages * p.b.stage_bytes, p.b, GGeo<K>::UW);
     return s;
 }
 
 __device__ __forceinline__ bool wait_all(uint64_t* bar, uint32_t parity, volatile WaitCtx* wc, bool ok)
 {
-    return __all_sync(0xffffffffu, ok && mbar_wait_short(bar, parity, wc));
+    return __all_sync(0xffffffffu, ok && mbar_wait(bar, parity, wc));
 }
 
 // The tiles of the block, in every role's own steps.
@@ -126,7 +137,7 @@ template <int K> __device__ __forceinline__ bool g_role(const RoleParams& p, Rol
 __device__ __forceinline__ bool load_barrier_and(bool ok)
 {
     int r;
-    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\tbarrier.cta.red.and.pred q, 3, %2, p;\n\tselp.b32 %0, 1, 0, q;\n\t}"
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\tbarrier.cta.red.and.pred q, 6, %2, p;\n\tselp.b32 %0, 1, 0, q;\n\t}"
                  : "=r"(r) : "r"((int)ok), "n"(kLoadThreads) : "memory");
     return r != 0;
 }
@@ -146,7 +157,7 @@ __device__ __forceinline__ void load_role(const CUtensorMap* map, const RolePara
         for (Tiles tl(p.b.g); tl.more(p.b.g) && ok; tl.next(p.b.g))
             for (int row = 0; row < tl.rows; ++row) {
                 const int item = tl.base + row, st = item % p.p_stages;
-                if (!(ok = mbar_wait_short(&ctl.p_empty[st], ((item / p.p_stages) & 1) ^ 1, wc))) break;
+                if (!(ok = mbar_wait(&ctl.p_empty[st], ((item / p.p_stages) & 1) ^ 1, wc))) break;
                 uint8_t* dst = sPhi + st * p.b.stage_bytes;
                 mbar_arrive_expect_tx(&ctl.p_full[st], (uint32_t)p.b.rows * 256u);
                 tma_load_4d(dst, map, &ctl.p_full[st], tl.x0, tl.y0 + row, 0, tl.f);
@@ -158,9 +169,33 @@ __device__ __forceinline__ void load_role(const CUtensorMap* map, const RolePara
             mbar_wait_drain(&ctl.p_full[item % p.p_stages], (item / p.p_stages) & 1);
         return;
     }
+    if (p.copy_bytes) {
+        // asynchronous copies of 16 or 4 bytes (eight pixels or two): planes picked one by one, widths and addresses TMA does not take
+        const int px = p.copy_bytes / 2, per = 128 / px, total = per * p.b.rows;
+        const bool pick = p.b.mode == kModeGlobal && !(pb.flags & SR_COEF_COMPACT);
+        bool go = true;
+        for (Tiles tl(p.b.g); tl.more(p.b.g) && go; tl.next(p.b.g))
+            for (int row = 0; row < tl.rows; ++row) {
+                const int item = tl.base + row, st = item % p.p_stages;
+                if (!(go = wait_all(&ctl.p_empty[st], ((item / p.p_stages) & 1) ^ 1, wc, go))) break;
+                const uint32_t stage = smem_u32(sPhi + st * p.b.stage_bytes);
+                const __half* src = p.b.coef + (int64_t)tl.f * p.planes_in * HW + (int64_t)(tl.y0 + row) * pb.W + tl.x0;
+                for (int i = tid; i < total; i += kLoadThreads) {
+                    const int l = i / per, x = (i - l * per) * px;       // (per is 16 or 64)
+                    const bool inside = tl.x0 + x < pb.W;
+                    const uint32_t dst = stage + (x >> 6) * p.b.chunk_bytes + l * 128 + ((((x & 63) >> 3) ^ (l & 7)) << 4) + (x & 7) * 2;
+                    const __half* from = src + (int64_t)(pick ? ctl.c.atoms[l] : l) * HW + (inside ? x : 0);
+                    if (px == 8) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(from), "r"(inside ? 16 : 0) : "memory");
+                    else asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(from), "r"(inside ? 4 : 0) : "memory");
+                }
+                asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(&ctl.p_full[st])) : "memory");
+            }
+        cp_async_wait_all_();
+        return;
+    }
     const int s = pb.s;
     const bool lists = p.b.mode == kModeIdx || p.b.mode == kModeCompact;
-    const bool gather = p.b.mode == kModeGlobal && !(pb.flags & SR_COEF_COMPACT);
+    const bool gather = p.b.mode == kModeGlobal && !(pb.flags & SR_COEF_COMPACT);      // (odd widths)
     const __half zero = __ushort_as_half(0);
     bool ok = true;
     for (Tiles tl(p.b.g); tl.more(p.b.g); tl.next(p.b.g)) {
@@ -195,13 +230,13 @@ __device__ __forceinline__ void load_role(const CUtensorMap* map, const RolePara
                             if (q0 + i < s) *place(a[i]) = v[i];
                     }
                 } else {
-                    for (int l0 = 0; l0 < p.b.rows; l0 += 24) {
-                        __half h[24];
+                    for (int l0 = 0; l0 < p.b.rows; l0 += 16) {
+                        __half h[16];
 #pragma unroll
-                        for (int i = 0; i < 24; ++i)
+                        for (int i = 0; i < 16; ++i)
                             h[i] = inside && l0 + i < p.b.rows ? __ldg(src + (int64_t)(gather ? ctl.c.atoms[l0 + i] : l0 + i) * HW) : zero;
 #pragma unroll
-                        for (int i = 0; i < 24; ++i)
+                        for (int i = 0; i < 16; ++i)
                             if (l0 + i < p.b.rows) *place(l0 + i) = h[i];
                     }
                 }
@@ -214,61 +249,57 @@ __device__ __forceinline__ void load_role(const CUtensorMap* map, const RolePara
 
 // ---- MMA warp -----------------------------------------------------------------------------------------------------------------
 
-template <int K> __device__ __forceinline__ void mma_role(const RoleParams& p, RoleCtl& ctl, const RoleSmem<K>& s, uint32_t tmem)
+// One warp a product: the issue of one row's instructions takes a single warp some thousand cycles on a busy multiprocessor.
+template <int K, bool COEF> __device__ __forceinline__ void mma_role(const RoleParams& p, RoleCtl& ctl, const RoleSmem<K>& s, uint32_t tmem)
 {
     using G = GGeo<K>;
     volatile WaitCtx* wc = &ctl.c.wait;
-    const uint64_t g_desc0 = make_smem_desc(smem_u32(s.G), 16, 1024, kSwizzle128B);              // rows: K-major
-    const uint64_t gt_desc0 = make_smem_desc(smem_u32(s.G), 128 * 128, 1024, kSwizzle128B);      // columns: MN-major
-    const uint64_t d_desc = make_smem_desc(smem_u32(s.D), 16, 1024, kSwizzle128B);
-    const uint64_t a_desc0 = make_smem_desc(smem_u32(s.Phi), 16, 1024, kSwizzle128B);
+    const uint64_t g_desc0 = COEF ? make_smem_desc(smem_u32(s.G), 16, 1024, kSwizzle128B)               // rows: K-major
+                                  : make_smem_desc(smem_u32(s.G), 128 * 128, 1024, kSwizzle128B);       // columns: MN-major
+    const uint64_t a_desc0 = make_smem_desc(smem_u32(COEF ? s.D : s.Phi), 16, 1024, kSwizzle128B);
     constexpr uint32_t kGLo = (G::BLOCKS == 2 ? 128 * 128 : G::LO_CHUNK * 16) >> 4;
-    constexpr uint32_t idesc_c = make_idesc_f16(128, 128, false, false), idesc_d = make_idesc_f16(128, G::NB, false, true);
-    bool lose = p.b.lose != 0 && blockIdx.x == 0;
+    const uint32_t kDLo = (uint32_t)(G::BLOCKS == 2 ? p.d_block : G::LO_CHUNK * 16) >> 4, a_chunk = (uint32_t)p.b.chunk_bytes >> 4;
+    constexpr uint32_t idesc = COEF ? make_idesc_f16(128, 128, false, false) : make_idesc_f16(128, G::NB, false, true);
+    bool lose = p.b.lose != 0 && blockIdx.x == 0 && (COEF || !p.want_coef);
     bool ok = true;
+    int gs = 0, ps = 0;                                      // ring entries of the row
+    uint32_t gp = 0, pp = 0;                                 // and the parities of their uses
     for (Tiles tl(p.b.g); tl.more(p.b.g) && ok; tl.next(p.b.g)) {
-        const uint32_t d_acc = tmem + 256 + (tl.n & 1) * G::NB;
         for (int row = 0; row < tl.rows; ++row) {
-            const int item = tl.base + row, gs = item % kRing<K>;
-            if (p.want_coef) ok = wait_all(&ctl.c_empty[item & 1], ((item >> 1) & 1) ^ 1, wc, ok);
-            if (p.want_dict && row == 0) ok = wait_all(&ctl.d_empty[tl.n & 1], ((tl.n >> 1) & 1) ^ 1, wc, ok);
-            ok = wait_all(&ctl.g_full[gs], (item / kRing<K>) & 1, wc, ok);
+            const int item = tl.base + row;
+            if (COEF) ok = wait_all(&ctl.c_empty[item & 1], ((item >> 1) & 1) ^ 1, wc, ok);
+            else if (row == 0) ok = wait_all(&ctl.d_empty[tl.n & 1], ((tl.n >> 1) & 1) ^ 1, wc, ok);
+            if (!COEF) ok = wait_all(&ctl.p_full[ps], pp, wc, ok);
+            ok = wait_all(&ctl.g_full[gs], gp, wc, ok);
             if (!ok) break;
+            if (!COEF && p.copy_bytes) fence_proxy_async_smem();         // (written by cp.async, read by the tensor core)
             tc_fence_after_sync();
-            const uint32_t g_off = (uint32_t)(gs * G::G_BYTES) >> 4;
-            if (p.want_coef) {
-                if (elect_one()) {
+            if (elect_one()) {
+                const uint64_t gd = g_desc0 + ((uint32_t)(gs * G::G_BYTES) >> 4);
+                if (COEF) {
                     const uint32_t acc = tmem + (item & 1) * 128;
 #pragma unroll
                     for (int ks = 0; ks < G::KSTEPS; ++ks) {
-                        const uint64_t gh = g_desc0 + g_off + 2 * ks, dh = d_desc + 2 * ks;
-                        mma_f16_ss(acc, dh, gh, idesc_c, ks > 0);
-                        mma_f16_ss(acc, dh, gh + kGLo, idesc_c, 1u);
-                        mma_f16_ss(acc, dh + kGLo, gh, idesc_c, 1u);
+                        mma_f16_ss(acc, a_desc0 + 2 * ks, gd + 2 * ks, idesc, ks > 0);
+                        mma_f16_ss(acc, a_desc0 + 2 * ks, gd + 2 * ks + kGLo, idesc, 1u);
+                        mma_f16_ss(acc, a_desc0 + 2 * ks + kDLo, gd + 2 * ks, idesc, 1u);
                     }
                     if (!lose) mma_commit(&ctl.c_full[item & 1]);
-                }
-                __syncwarp();
-            }
-            if (p.want_dict) {
-                const int ps = item % p.p_stages;
-                ok = wait_all(&ctl.p_full[ps], (item / p.p_stages) & 1, wc, ok);
-                if (!ok) break;
-                tc_fence_after_sync();
-                if (elect_one()) {
-                    const uint32_t a_off = (uint32_t)(ps * p.b.stage_bytes) >> 4, a_chunk = (uint32_t)p.b.chunk_bytes >> 4;
+                } else {
+                    const uint32_t acc = tmem + 256 + (tl.n & 1) * G::NB;
+                    const uint64_t ad = a_desc0 + ((uint32_t)(ps * p.b.stage_bytes) >> 4);
 #pragma unroll
                     for (int ks = 0; ks < 8; ++ks)
-                        mma_f16_ss(d_acc, a_desc0 + a_off + (ks >> 2) * a_chunk + (ks & 3) * 2, gt_desc0 + g_off + (uint32_t)(ks * 2048 >> 4), idesc_d,
-                                   row > 0 || ks > 0);
-                    if (!(lose && !p.want_coef)) mma_commit(&ctl.p_empty[ps]);
+                        mma_f16_ss(acc, ad + (ks >> 2) * a_chunk + (ks & 3) * 2, gd + (uint32_t)(ks * 2048 >> 4), idesc, row > 0 || ks > 0);
+                    if (!lose) mma_commit(&ctl.p_empty[ps]);
                     if (row == tl.rows - 1) mma_commit(&ctl.d_full[tl.n & 1]);
                 }
-                __syncwarp();
+                mma_commit(&ctl.g_empty[gs]);
             }
-            if (elect_one()) mma_commit(&ctl.g_empty[gs]);
             __syncwarp();
             lose = false;
+            if (++gs == kRing<K>) { gs = 0; gp ^= 1; }
+            if (++ps == p.p_stages) { ps = 0; pp ^= 1; }
         }
     }
     // tensor memory is freed only once every product has finished
@@ -278,16 +309,15 @@ template <int K> __device__ __forceinline__ void mma_role(const RoleParams& p, R
 
 // ---- result warps ---------------------------------------------------------------------------------------------------------------
 
-__device__ __forceinline__ bool result_barrier(bool ok) { return group_barrier_and(2, ok); }
-
-template <int K> __device__ __forceinline__ void result_role(const CUtensorMap* map, const RoleParams& p, RoleCtl& ctl, const RoleSmem<K>& s, uint32_t tmem, int tid)
+template <int K> __device__ __forceinline__ void result_role(const CUtensorMap* map, const RoleParams& p, RoleCtl& ctl, const RoleSmem<K>& s, uint32_t tmem, int grp, int tid)
 {
     using G = GGeo<K>;
     const Problem& pb = p.b.g.pb;
     volatile WaitCtx* wc = &ctl.c.wait;
+    auto result_barrier = [&](bool go) { return group_barrier_and(2 + grp, go); };
     const int warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31, l = 32 * warp + lane, W = pb.W;
     const int64_t HW = (int64_t)pb.H * W;
-    const uint32_t at = tmem + ((uint32_t)(32 * warp) << 16);
+    const uint32_t at = tmem + ((uint32_t)(32 * warp) << 16), acc_at = at + grp * 128;
     constexpr int STEP = K == 7 ? 16 : 32;                   // accumulator columns at a time (registers)
     const bool listed = p.b.mode == kModeIdx, compact = p.b.mode == kModeCompact;
     const bool together = p.want_coef && (listed || compact);        // these meet at barriers, so they leave together
@@ -296,76 +326,74 @@ template <int K> __device__ __forceinline__ void result_role(const CUtensorMap* 
     float total[G::kk];
 #pragma unroll
     for (int j = 0; j < G::kk; ++j) total[j] = 0.f;
+    uint8_t* chunk = s.out + grp * kOutBytes;                // 64 pixels of the group's 128 atoms
+    uint8_t* to = chunk + warp * 4096;
     bool ok = true;
-    int buffer = 0;
     for (Tiles tl(p.b.g); tl.more(p.b.g) && ok; tl.next(p.b.g)) {
-        for (int row = 0; p.want_coef && row < tl.rows; ++row) {
+        for (int row = (tl.base + grp) & 1; p.want_coef && row < tl.rows; row += kRG) {      // rows whose number is grp modulo 2
             const int item = tl.base + row;
             const int64_t pix = (int64_t)(tl.y0 + row) * W + tl.x0;
             uint32_t keep[4] = {~0u, ~0u, ~0u, ~0u};
             if (listed) {                                    // which of the row's pixels list this lane's atom
                 if (!(ok = result_barrier(ok))) break;       // the row before has been read
 #pragma unroll
-                for (int i = 0; i < 4; ++i) ctl.listed[tid][i] = 0u;
+                for (int i = 0; i < 4; ++i) ctl.listed[grp][tid][i] = 0u;
                 if (!(ok = result_barrier(ok))) break;
                 if (tl.x0 + tid < W)
                     for (int q = 0; q < pb.s; ++q) {
                         const int a = min((int)__ldg(p.b.idx + ((int64_t)tl.f * pb.s + q) * HW + pix + tid), pb.D - 1);
-                        atomicOr(&ctl.listed[a][tid >> 5], 1u << (tid & 31));
+                        atomicOr(&ctl.listed[grp][a][tid >> 5], 1u << (tid & 31));
                     }
             }
-            ok = wait_all(&ctl.c_full[item & 1], (item >> 1) & 1, wc, ok);
+            ok = wait_all(&ctl.c_full[grp], (item >> 1) & 1, wc, ok);
             if (listed) {
                 if (!(ok = result_barrier(ok))) break;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) keep[i] = ctl.listed[l][i];
+                for (int i = 0; i < 4; ++i) keep[i] = ctl.listed[grp][l][i];
             }
             tc_fence_after_sync();
             const float k = back * *(volatile float*)&ctl.unscale[tl.n % kUnscales];
 #pragma unroll
             for (int c0 = 0; c0 < 128; c0 += 64) {
-                uint32_t h[32];
-                uint8_t* to = s.out + buffer * kOutBytes + warp * 4096;
-                if (mine && ok) {
+                if (compact) {
+                    if (!(ok = result_barrier(ok))) break;   // the chunk before has been taken
+                }
 #pragma unroll
-                    for (int c1 = 0; c1 < 64; c1 += STEP) {
-                        float acc[STEP];
+                for (int c1 = 0; c1 < 64; c1 += STEP) {
+                    float acc[STEP];
+                    if (mine && ok) {
 #pragma unroll
-                        for (int i = 0; i < STEP; i += 16) tmem_ld_x16(at + (item & 1) * 128 + c0 + c1 + i, acc + i);
+                        for (int i = 0; i < STEP; i += 16) tmem_ld_x16(acc_at + c0 + c1 + i, acc + i);
+                    }
+                    if (c1 == 0 && !compact) {
+                        if (lane == 0) bulk_wait_read();     // the store before has read the buffer
+                        __syncwarp();
+                    }
+                    if (mine && ok) {
                         tmem_ld_wait();
 #pragma unroll
-                        for (int i = 0; i < STEP / 2; ++i) {
-                            const __half2 v2 = __floats2half2_rn(acc[2 * i] * k, acc[2 * i + 1] * k);
-                            h[c1 / 2 + i] = *reinterpret_cast<const uint32_t*>(&v2);
-                        }
-                    }
-                    if (back == 0.f) {                       // outside the subset: zeros, whatever G is
+                        for (int j = 0; j < STEP / 8; ++j) {
+                            uint32_t h[4];
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) h[i] = 0u;
-                    }
-                    if (listed) {
+                            for (int i = 0; i < 4; ++i) {
+                                const __half2 v2 = __floats2half2_rn(acc[8 * j + 2 * i] * k, acc[8 * j + 2 * i + 1] * k);
+                                h[i] = back != 0.f ? *reinterpret_cast<const uint32_t*>(&v2) : 0u;   // (outside the subset: zeros, whatever G is)
+                            }
+                            if (listed) {
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) {
-                            const uint32_t two = keep[(c0 + 2 * i) / 32] >> ((c0 + 2 * i) % 32);
-                            h[i] &= ((two & 1u) ? 0xFFFFu : 0u) | ((two & 2u) ? 0xFFFF0000u : 0u);
+                                for (int i = 0; i < 4; ++i) {
+                                    const uint32_t two = keep[(c0 + c1 + 8 * j + 2 * i) / 32] >> ((c0 + c1 + 8 * j + 2 * i) % 32);
+                                    h[i] &= ((two & 1u) ? 0xFFFFu : 0u) | ((two & 2u) ? 0xFFFF0000u : 0u);
+                                }
+                            }
+                            *reinterpret_cast<uint4*>(to + lane * 128 + (((c1 / 8 + j) ^ (lane & 7)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
                         }
                     }
                 }
                 if (c0 == 64) {                              // the accumulator has been read
                     tc_fence_before_sync();
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(&ctl.c_empty[item & 1]);
-                }
-                if (compact) {
-                    if (!(ok = result_barrier(ok))) break;   // the buffer's values two chunks ago have been taken
-                } else {
-                    if (lane == 0) bulk_wait_read_but_one(); // the store two chunks ago has read the buffer
-                    __syncwarp();
-                }
-                if (mine && ok) {
-#pragma unroll
-                    for (int j = 0; j < 8; ++j)
-                        *reinterpret_cast<uint4*>(to + lane * 128 + ((j ^ (lane & 7)) << 4)) = make_uint4(h[4 * j], h[4 * j + 1], h[4 * j + 2], h[4 * j + 3]);
+                    if (lane == 0) mbar_arrive(&ctl.c_empty[grp]);
                 }
                 if (compact) {
                     // values by rank: a pixel's listed atoms out of the chunk
@@ -375,14 +403,16 @@ template <int K> __device__ __forceinline__ void result_role(const CUtensorMap* 
                         for (int q = tid >> 6; q < pb.s; q += 2) {
                             const int64_t pl = ((int64_t)tl.f * pb.s + q) * HW + pix + c0 + px;
                             const int a = min((int)__ldg(p.b.idx + pl), pb.D - 1);
-                            p.b.gcoef[pl] = *reinterpret_cast<const __half*>(s.out + buffer * kOutBytes + (a >> 5) * 4096 + (a & 31) * 128 +
+                            p.b.gcoef[pl] = *reinterpret_cast<const __half*>(chunk + (a >> 5) * 4096 + (a & 31) * 128 +
                                                                             ((((px >> 3) ^ (a & 7))) << 4) + (px & 7) * 2);
                         }
                 } else if (p.tma_out) {
                     fence_proxy_async_smem();
                     __syncwarp();
-                    if (lane == 0 && mine && ok && tl.x0 + c0 < W) tma_store_4d(map, to, tl.x0 + c0, tl.y0 + row, 32 * warp, tl.f);
-                    if (lane == 0) bulk_commit();            // (an empty group where nothing was stored: groups are counted)
+                    if (lane == 0 && mine && ok && tl.x0 + c0 < W) {
+                        tma_store_4d(map, to, tl.x0 + c0, tl.y0 + row, 32 * warp, tl.f);
+                        bulk_commit();
+                    }
                 } else if (mine && ok) {
                     // any alignment: a plane's 64 pixels a warp, two elements a lane
                     __syncwarp();
@@ -396,11 +426,10 @@ template <int K> __device__ __forceinline__ void result_role(const CUtensorMap* 
                     }
                     __syncwarp();
                 }
-                buffer ^= 1;
             }
             if (!ok) break;
         }
-        if (p.want_dict && ok) {
+        if (p.want_dict && grp == 0 && ok) {
             ok = wait_all(&ctl.d_full[tl.n & 1], (tl.n >> 1) & 1, wc, ok);
             if (together) ok = result_barrier(ok);
             tc_fence_after_sync();
@@ -425,7 +454,7 @@ template <int K> __device__ __forceinline__ void result_role(const CUtensorMap* 
         }
     }
     if (lane == 0) bulk_wait_all();
-    if (p.want_dict && l < p.b.rows) {
+    if (p.want_dict && grp == 0 && l < p.b.rows) {
         float* out = p.b.partial + ((int64_t)blockIdx.x * p.b.rows + l) * G::kk;
 #pragma unroll
         for (int j = 0; j < G::kk; ++j) out[j] = total[j];
@@ -444,9 +473,9 @@ grad_roles_kernel(const __grid_constant__ CUtensorMap map_in, const __grid_const
     const Problem& pb = p.b.g.pb;
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), D = pb.D;
 
-    init_ctl(ctl.c, p.b, tid, kRoleThreads, 1);
+    init_ctl(ctl.c, p.b, tid, kRoleThreads, p.want_coef + p.want_dict);
     if (tid == 0) {
-        for (int i = 0; i < kMaxG; ++i) { mbar_init(&ctl.g_full[i], kGroupThreads); mbar_init(&ctl.g_empty[i], 1); }
+        for (int i = 0; i < kMaxG; ++i) { mbar_init(&ctl.g_full[i], kGroupThreads); mbar_init(&ctl.g_empty[i], p.want_coef + p.want_dict); }
         for (int i = 0; i < kMaxP; ++i) { mbar_init(&ctl.p_full[i], p.tma_in ? 1 : kLoadThreads); mbar_init(&ctl.p_empty[i], 1); }
         for (int i = 0; i < 2; ++i) { mbar_init(&ctl.c_full[i], 1); mbar_init(&ctl.c_empty[i], 4); mbar_init(&ctl.d_full[i], 1); mbar_init(&ctl.d_empty[i], 4); }
         fence_barrier_init();
@@ -458,7 +487,7 @@ grad_roles_kernel(const __grid_constant__ CUtensorMap map_in, const __grid_const
     if (p.b.mode == kModeGlobal && tid < pb.s) ctl.c.atoms[tid] = (uint8_t)min((int)__ldg(p.b.idx + tid), D - 1);
     __syncthreads();
     if (p.want_coef)
-        for (int q = tid; q < p.atoms; q += kRoleThreads) ctl.back[q] = write_atom<K>(p.b, s.D, 128 * 128, q);
+        for (int q = tid; q < p.atoms; q += kRoleThreads) ctl.back[q] = write_atom<K>(p.b, s.D, p.d_block, q);
     fence_proxy_async_smem();
     if (warp == kMmaWarp) tmem_alloc(&ctl.c.tmem_base, 512);
     tc_fence_before_sync();
@@ -466,10 +495,19 @@ grad_roles_kernel(const __grid_constant__ CUtensorMap map_in, const __grid_const
     tc_fence_after_sync();
     const uint32_t tmem = ctl.c.tmem_base;
 
-    if (warp < kResultWarp) g_role<K>(p, ctl, s, tid);
-    else if (warp < kLoadWarp) result_role<K>(&map_out, p, ctl, s, tmem, tid - kResultWarp * 32);
-    else if (warp < kMmaWarp) { if (p.want_dict) load_role(&map_in, p, ctl, s.Phi, tid - kLoadWarp * 32); }
-    else mma_role<K>(p, ctl, s, tmem);
+    // (setmaxnreg: whole warpgroups)
+    if (warp < kResultWarp) {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsG));
+        g_role<K>(p, ctl, s, tid);
+    } else if (warp < kLoadWarp) {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsResult));
+        result_role<K>(&map_out, p, ctl, s, tmem, (warp - kResultWarp) / 4, (tid - kResultWarp * 32) % kGroupThreads);
+    } else {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsLoad));
+        if (warp == kMmaWarp) { if (p.want_coef) mma_role<K, true>(p, ctl, s, tmem); }
+        else if (warp == kMmaWarp + 1) { if (p.want_dict) mma_role<K, false>(p, ctl, s, tmem); }
+        else if (p.want_dict) load_role(&map_in, p, ctl, s.Phi, tid - kLoadWarp * 32);
+    }
 
     __syncwarp();
     tc_fence_before_sync();
@@ -490,11 +528,13 @@ template <int K> bool plan(RoleParams& p, const GradArgs& a, size_t& smem)
     p.want_coef = a.gcoef != nullptr;
     p.want_dict = a.gdict || a.ggamma;
     p.atoms = product_atoms(a);
+    p.d_block = ((p.atoms + 7) & ~7) * 128;              // (the product reads 128 rows; those behind are whatever follows)
     p.b.rows = grad_rows(a);
     p.b.stage_bytes = stage_bytes_of(p.b.rows);
     p.b.chunk_bytes = p.b.stage_bytes / 2;
     const size_t floats = float_bytes<K>(p.b.g, a.pb, a.lr);
-    const size_t fixed = 1024 + (size_t)kRing<K> * GGeo<K>::G_BYTES + (p.want_coef ? GGeo<K>::BLOCKS * 128 * 128 + 2 * kOutBytes : 0) + floats;
+    // (behind the atoms lie 16 KB and more of results, so what the first product reads there is shared memory)
+    const size_t fixed = 1024 + (size_t)kRing<K> * GGeo<K>::G_BYTES + (p.want_coef ? GGeo<K>::BLOCKS * p.d_block + kRG * kOutBytes : 0) + floats;
     p.p_stages = 0;
     smem = fixed;
     if (p.want_dict) {
@@ -503,11 +543,11 @@ template <int K> bool plan(RoleParams& p, const GradArgs& a, size_t& smem)
             // the second product reads 128 rows of a chunk, whatever lies behind the last one must be shared memory
             const size_t reach = smem - floats - p.b.chunk_bytes + 128 * 128;
             if (smem < reach) smem = reach;
-            if (fits(smem)) break;
+            if (fits(smem, kRoleReserve)) break;
         }
         if (p.p_stages < 2) return false;
     }
-    return fits(smem);
+    return fits(smem, kRoleReserve);
 }
 
 template <int K> cudaError_t launch_k(const GradArgs& a, int* slots)
@@ -523,9 +563,11 @@ template <int K> cudaError_t launch_k(const GradArgs& a, int* slots)
     const Problem& pb = a.pb;
     const bool whole = a.mode == kModeDense || (a.mode == kModeGlobal && (pb.flags & SR_COEF_COMPACT));
     if (p.want_dict && whole && pb.W % 8 == 0 && ((uintptr_t)a.coef & 15) == 0) p.tma_in = encode_planes(&in, a.coef, pb, p.planes_in, p.b.rows);
+    if (p.want_dict && !p.tma_in && (whole || a.mode == kModeGlobal))
+        p.copy_bytes = pb.W % 8 == 0 && ((uintptr_t)a.coef & 15) == 0 ? 16 : (pb.W % 2 == 0 && ((uintptr_t)a.coef & 3) == 0 ? 4 : 0);
     if (p.want_coef && a.mode != kModeCompact && pb.W % 8 == 0 && ((uintptr_t)a.gcoef & 15) == 0) p.tma_out = encode_planes(&out, a.gcoef, pb, p.planes_out, 32);
     static bool done[64] = {false};
-    if (cudaError_t e = allow_smem(grad_roles_kernel<K>, done)) return e;
+    if (cudaError_t e = allow_smem(grad_roles_kernel<K>, done, kRoleReserve)) return e;
     const int blocks = p.b.g.num_tiles < sm_count() ? p.b.g.num_tiles : sm_count();
     grad_roles_kernel<K><<<blocks, kRoleThreads, smem, a.st>>>(in, out, p);
     count_launches(1);

@@ -171,8 +171,7 @@ template <int NT, bool NAMED> __device__ __forceinline__ void makers_sync()
 // The up-sampled tile, the pixel's grad_out values of the group's rows and the tile's scale; made by NG groups.
 template <int K, int NG, bool NAMED> struct TileState {
     using G = GGeo<K>;
-    static constexpr int NT = NG * kGroupThreads, ROWS = kMaxTH / NG;
-    static_assert(ROWS * NG == kMaxTH, "the groups share a tile's rows evenly");
+    static constexpr int NT = NG * kGroupThreads, ROWS = (kMaxTH + NG - 1) / NG;
     LrWindow w;                                  // of the tile in work
     float next_g[ROWS][kMaxC];                   // grad_out of the next tile's rows, asked for a tile ahead
     float scale, unscale;
@@ -223,7 +222,7 @@ template <int K, int NG, bool NAMED> struct TileState {
         for (int i = 0; i < ROWS; ++i)
 #pragma unroll
             for (int c = 0; c < kMaxC; ++c) {
-                if (c < C) {
+                if (c < C && (kMaxTH % NG == 0 || first + NG * i < kMaxTH)) {
                     s.g[((first + NG * i) * C + c) * kGroupThreads + x] = next_g[i][c];
                     top_g = max(top_g, finite_bits(next_g[i][c]));
                 }
@@ -371,12 +370,12 @@ template <int K> size_t float_bytes(Geom& g, const Problem& pb, const float* lr)
     return (plan_geom(g, pb, tile_rows(pb), lr) + 8 + (size_t)kMaxTH * pb.c * kGroupThreads) * sizeof(float);
 }
 
-template <typename Kern> cudaError_t allow_smem(Kern kern, bool (&done)[64])
+template <typename Kern> cudaError_t allow_smem(Kern kern, bool (&done)[64], int reserve = kStaticReserve)
 {
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
     if (!done[dev]) {
-        if (cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_optin() - kStaticReserve)) return e;
+        if (cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_optin() - reserve)) return e;
         done[dev] = true;
     }
     return cudaSuccess;
@@ -417,7 +416,7 @@ inline bool form_supported(const GradArgs& a)
            (int64_t)((pb.W + TW - 1) / TW) * ((pb.H + 1) / 2) * pb.n <= 0x7FFFFFFF;
 }
 
-inline bool fits(size_t smem) { return smem + kStaticReserve <= (size_t)smem_optin(); }
+inline bool fits(size_t smem, int reserve = kStaticReserve) { return smem + reserve <= (size_t)smem_optin(); }
 
 } // namespace gradtc
 } // namespace sr
