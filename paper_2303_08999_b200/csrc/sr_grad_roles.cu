@@ -81,21 +81,6 @@ __device__ __forceinline__ bool wait_all(uint64_t* bar, uint32_t parity, volatil
     return __all_sync(0xffffffffu, ok && mbar_wait(bar, parity, wc));
 }
 
-// The tiles of the block, in every role's own steps.
-struct Tiles {
-    int t, base, n;                                          // tile, number of its first row, number of the tile
-    int f, y0, x0, rows;
-    __device__ __forceinline__ explicit Tiles(const Geom& g) : t(blockIdx.x), base(0), n(0) { if (more(g)) decode_tile(g, t, f, y0, x0, rows); }
-    __device__ __forceinline__ bool more(const Geom& g) const { return t < g.num_tiles; }
-    __device__ __forceinline__ void next(const Geom& g)
-    {
-        base += rows;
-        ++n;
-        t += gridDim.x;
-        if (more(g)) decode_tile(g, t, f, y0, x0, rows);
-    }
-};
-
 // ---- G warps ----------------------------------------------------------------------------------------------------------------
 
 template <int K> __device__ __forceinline__ bool g_role(const RoleParams& p, RoleCtl& ctl, const RoleSmem<K>& s, int tid)
@@ -105,30 +90,28 @@ template <int K> __device__ __forceinline__ bool g_role(const RoleParams& p, Rol
     volatile WaitCtx* wc = &ctl.c.wait;
     TileState<K, kFG, true> ts;
     Tiles tl(p.b.g);
-    ts.start(p.b, s.f, tid, grp);                            // (row `grp` is the group's first of the block)
+    ts.start(p.b, tl, s.f, tid, grp);                            // (row `grp` is the group's first of the block)
     bool ok = true;
     int parity = 0;
     for (; tl.more(p.b.g); parity ^= 1) {
-        const int first = (grp + kFG - tl.base % kFG) % kFG;             // the group's first row of the tile
-        Tiles after = tl;
-        after.next(p.b.g);
-        const int next_first = (grp + kFG - after.base % kFG) % kFG;
-        if (!(ok = ts.make(p.b, ctl.c, tl.t, parity, s.f, tid, ok, first, next_first, &ctl.unscale[tl.n % kUnscales]))) break;
+        const int base = tl.base, rows = tl.rows, n = tl.n;
         const bool inside = tl.x0 + x < p.b.g.pb.W;
-        for (int row = first; row < tl.rows; row += kFG) {
+        const int first = (grp + kFG - base % kFG) % kFG;                // the group's first row of the tile
+        tl.next(p.b.g);                                                  // (the tile after it is asked for while this one is made)
+        if (!(ok = ts.make(p.b, ctl.c, tl, parity, s.f, tid, ok, first, (grp + kFG - tl.base % kFG) % kFG, &ctl.unscale[n % kUnscales]))) break;
+        for (int row = first; row < rows; row += kFG) {
             float v[G::kk];
             patch_grad<K>(s.f.U + row * G::UW + x, p.b.g.uh * G::UW, s.f.g + row * C * kGroupThreads + x, C, ts.scale, v, [] {});
             if (!inside) {
 #pragma unroll
                 for (int j = 0; j < G::kk; ++j) v[j] = 0.f;              // (patches of columns beyond the image may be anything)
             }
-            const int item = tl.base + row, st = item % kRing<K>;
+            const int item = base + row, st = item % kRing<K>;
             ok = wait_all(&ctl.g_empty[st], ((item / kRing<K>) & 1) ^ 1, wc, ok);
             if (ok) write_row<K>(s.G + st * G::G_BYTES, 128 * 128, x, v);
             fence_proxy_async_smem();
             mbar_arrive(&ctl.g_full[st]);
         }
-        tl = after;
     }
     cp_async_wait_all_();
     return ok;
@@ -320,6 +303,7 @@ template <int K> __device__ __forceinline__ void result_role(const CUtensorMap* 
     const uint32_t at = tmem + ((uint32_t)(32 * warp) << 16), acc_at = at + grp * 128;
     constexpr int STEP = K == 7 ? 16 : 32;                   // accumulator columns at a time (registers)
     const bool listed = p.b.mode == kModeIdx, compact = p.b.mode == kModeCompact;
+    const bool masked = listed || (p.b.mode == kModeGlobal && !(pb.flags & SR_COEF_COMPACT));
     const bool together = p.want_coef && (listed || compact);        // these meet at barriers, so they leave together
     const bool mine = 32 * warp < p.atoms;                   // this warp has atoms
     const float back = p.want_coef && l < p.atoms ? ctl.back[l] : 0.f;
@@ -333,7 +317,8 @@ template <int K> __device__ __forceinline__ void result_role(const CUtensorMap* 
         for (int row = (tl.base + grp) & 1; p.want_coef && row < tl.rows; row += kRG) {      // rows whose number is grp modulo 2
             const int item = tl.base + row;
             const int64_t pix = (int64_t)(tl.y0 + row) * W + tl.x0;
-            uint32_t keep[4] = {~0u, ~0u, ~0u, ~0u};
+            const uint32_t whole = back != 0.f ? ~0u : 0u;
+            uint32_t keep[4] = {whole, whole, whole, whole};
             if (listed) {                                    // which of the row's pixels list this lane's atom
                 if (!(ok = result_barrier(ok))) break;       // the row before has been read
 #pragma unroll
@@ -349,7 +334,7 @@ template <int K> __device__ __forceinline__ void result_role(const CUtensorMap* 
             if (listed) {
                 if (!(ok = result_barrier(ok))) break;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) keep[i] = ctl.listed[grp][l][i];
+                for (int i = 0; i < 4; ++i) keep[i] &= ctl.listed[grp][l][i];
             }
             tc_fence_after_sync();
             const float k = back * *(volatile float*)&ctl.unscale[tl.n % kUnscales];
@@ -377,9 +362,9 @@ template <int K> __device__ __forceinline__ void result_role(const CUtensorMap* 
 #pragma unroll
                             for (int i = 0; i < 4; ++i) {
                                 const __half2 v2 = __floats2half2_rn(acc[8 * j + 2 * i] * k, acc[8 * j + 2 * i + 1] * k);
-                                h[i] = back != 0.f ? *reinterpret_cast<const uint32_t*>(&v2) : 0u;   // (outside the subset: zeros, whatever G is)
+                                h[i] = *reinterpret_cast<const uint32_t*>(&v2);
                             }
-                            if (listed) {
+                            if (masked) {                    // pixels that do not list the atom, an atom outside the subset: zeros, whatever G is
 #pragma unroll
                                 for (int i = 0; i < 4; ++i) {
                                     const uint32_t two = keep[(c0 + c1 + 8 * j + 2 * i) / 32] >> ((c0 + c1 + 8 * j + 2 * i) % 32);

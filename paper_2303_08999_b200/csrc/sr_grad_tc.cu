@@ -59,7 +59,8 @@ grad_coef_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_consta
     for (int i = tid; i < p.g.pb.c * p.g.trows * p.g.tcols + 8; i += kThreads) s.L[i] = 0.f;
     __syncthreads();
     TileState<K, kGroups, false> ts;
-    ts.start(p, s, tid, grp);
+    Tiles tl(p.g);
+    ts.start(p, tl, s, tid, grp);
     for (int q = tid; q < p.rows; q += kThreads) sback[q] = write_atom<K>(p, sD, d_block, q);
     fence_proxy_async_smem();
     if (warp == 0) tmem_alloc(&ctl.tmem_base, kGroups * 128);
@@ -77,9 +78,10 @@ grad_coef_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_consta
     uint32_t phase = 0;
     bool ok = true;
     int parity = 0;
-    for (int t = blockIdx.x; t < p.g.num_tiles; t += gridDim.x, parity ^= 1) {
+    for (; tl.more(p.g); parity ^= 1) {
+        tl.next(p.g);                            // (the tile after the one in work)
         const LrWindow w = ts.w;
-        if (!(ok = ts.make(p, ctl, t, parity, s, tid, ok, grp, grp, nullptr))) break;
+        if (!(ok = ts.make(p, ctl, tl, parity, s, tid, ok, grp, grp, nullptr))) break;
         const bool inside = w.x0 + x < W;
         const uint32_t at = tmem + ((uint32_t)(32 * (warp & 3)) << 16);
         auto multiply = [&](int m0) {            // thread 0 of the group: planes m0 .. m0 + 127 of the row in sG
@@ -241,7 +243,8 @@ grad_dict_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_consta
     volatile WaitCtx* wc = &ctl.wait;
     const int64_t HW = (int64_t)pb.H * W;
     TileState<K, kGroups, false> ts;
-    ts.start(p, s, tid, grp);
+    Tiles tl(p.g);
+    ts.start(p, tl, s, tid, grp);
     const uint64_t g_desc = make_smem_desc(smem_u32(sG), 128 * 128, 1024, kSwizzle128B);
     const uint64_t a_desc = make_smem_desc(smem_u32(sPhi), 16, 1024, kSwizzle128B);
     constexpr uint32_t idesc = make_idesc_f16(128, G::NB, false, true);
@@ -260,7 +263,8 @@ grad_dict_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_consta
     uint8_t* chunk = sPhi + (x >> 6) * p.chunk_bytes;
     const int unit = (x & 63) >> 3, at2 = (x & 7) * 2;                         // this pixel's 16-byte unit and place in it
     auto place = [&](int l) { return reinterpret_cast<__half*>(chunk + l * 128 + ((unit ^ (l & 7)) << 4) + at2); };
-    for (int t = blockIdx.x; t < p.g.num_tiles; t += gridDim.x, parity ^= 1) {
+    for (; tl.more(p.g); parity ^= 1) {
+        tl.next(p.g);                            // (the tile after the one in work)
         const LrWindow w = ts.w;
         auto fetch = [&](int row) {              // the group's first warp: two boxes, bytes counted on full
             landing = true;
@@ -271,7 +275,7 @@ grad_dict_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_consta
         };
         if (p.tma && leads && grp < w.rows && ok) fetch(grp);                  // (the tile before was waited for at its end)
         __syncwarp();
-        if (!(ok = ts.make(p, ctl, t, parity, s, tid, ok, grp, grp, nullptr))) break;
+        if (!(ok = ts.make(p, ctl, tl, parity, s, tid, ok, grp, grp, nullptr))) break;
         const bool inside = w.x0 + x < W;
         for (int row = grp; row < w.rows; row += kGroups) {
             float v[G::kk];
