@@ -290,6 +290,13 @@ template <int K, bool COEF> __device__ __forceinline__ void mma_role(const RoleP
     __syncwarp();
 }
 
+// Two products with one factor, packed.
+__device__ __forceinline__ void times2(float& x, float& y, float a, float b, float k)
+{
+    asm("{\n\t.reg .b64 v, f;\n\tmov.b64 v, {%2, %3};\n\tmov.b64 f, {%4, %4};\n\tmul.rn.f32x2 v, v, f;\n\tmov.b64 {%0, %1}, v;\n\t}"
+        : "=f"(x), "=f"(y) : "f"(a), "f"(b), "f"(k));
+}
+
 // ---- result warps ---------------------------------------------------------------------------------------------------------------
 
 template <int K> __device__ __forceinline__ void result_role(const CUtensorMap* map, const RoleParams& p, RoleCtl& ctl, const RoleSmem<K>& s, uint32_t tmem, int grp, int tid)
@@ -303,7 +310,6 @@ template <int K> __device__ __forceinline__ void result_role(const CUtensorMap* 
     const uint32_t at = tmem + ((uint32_t)(32 * warp) << 16), acc_at = at + grp * 128;
     constexpr int STEP = K == 7 ? 16 : 32;                   // accumulator columns at a time (registers)
     const bool listed = p.b.mode == kModeIdx, compact = p.b.mode == kModeCompact;
-    const bool masked = listed || (p.b.mode == kModeGlobal && !(pb.flags & SR_COEF_COMPACT));
     const bool together = p.want_coef && (listed || compact);        // these meet at barriers, so they leave together
     const bool mine = 32 * warp < p.atoms;                   // this warp has atoms
     const float back = p.want_coef && l < p.atoms ? ctl.back[l] : 0.f;
@@ -318,7 +324,7 @@ template <int K> __device__ __forceinline__ void result_role(const CUtensorMap* 
             const int item = tl.base + row;
             const int64_t pix = (int64_t)(tl.y0 + row) * W + tl.x0;
             const uint32_t whole = back != 0.f ? ~0u : 0u;
-            uint32_t keep[4] = {whole, whole, whole, whole};
+            uint32_t keep[4] = {0u, 0u, 0u, 0u};
             if (listed) {                                    // which of the row's pixels list this lane's atom
                 if (!(ok = result_barrier(ok))) break;       // the row before has been read
 #pragma unroll
@@ -334,7 +340,7 @@ template <int K> __device__ __forceinline__ void result_role(const CUtensorMap* 
             if (listed) {
                 if (!(ok = result_barrier(ok))) break;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) keep[i] &= ctl.listed[grp][l][i];
+                for (int i = 0; i < 4; ++i) keep[i] = ctl.listed[grp][l][i];
             }
             tc_fence_after_sync();
             const float k = back * *(volatile float*)&ctl.unscale[tl.n % kUnscales];
@@ -361,10 +367,12 @@ template <int K> __device__ __forceinline__ void result_role(const CUtensorMap* 
                             uint32_t h[4];
 #pragma unroll
                             for (int i = 0; i < 4; ++i) {
-                                const __half2 v2 = __floats2half2_rn(acc[8 * j + 2 * i] * k, acc[8 * j + 2 * i + 1] * k);
-                                h[i] = *reinterpret_cast<const uint32_t*>(&v2);
+                                float a, b;
+                                times2(a, b, acc[8 * j + 2 * i], acc[8 * j + 2 * i + 1], k);
+                                const __half2 v2 = __floats2half2_rn(a, b);
+                                h[i] = *reinterpret_cast<const uint32_t*>(&v2) & whole;      // (an atom outside the subset: zeros, whatever G is)
                             }
-                            if (masked) {                    // pixels that do not list the atom, an atom outside the subset: zeros, whatever G is
+                            if (listed) {                    // pixels that do not list the atom
 #pragma unroll
                                 for (int i = 0; i < 4; ++i) {
                                     const uint32_t two = keep[(c0 + c1 + 8 * j + 2 * i) / 32] >> ((c0 + c1 + 8 * j + 2 * i) % 32);
