@@ -18,18 +18,54 @@ constexpr int TX = 32, CCHUNK = 4;
 // The D k^2 multiply-adds of a pixel.
 template <int K> struct KK { static constexpr int value = K * K, padded = (K * K + 3) & ~3; };
 
-// Up-sampled tile of channels c0 .. c0 + nc - 1 with its halo, in shared memory.
-template <int K, int TY>
-__device__ __forceinline__ void fill_u(const float* __restrict__ lr, float* sU, const Problem& pb, int f, int c0, int nc, int X0, int Y0, int tid, int nthr)
-{
-    constexpr int P = (K - 1) / 2, UW = TX + 2 * P, UH = TY + 2 * P;
-    for (int i = tid; i < nc * UH * UW; i += nthr) {
-        const int ch = i / (UH * UW), rem = i - ch * (UH * UW);
-        const int uy = rem / UW, ux = rem - uy * UW;
-        const float* plane = lr + ((int64_t)f * pb.c + c0 + ch) * pb.h * pb.w;
-        sU[i] = bicubic_point(plane, pb.h, pb.w, pb.r, pb.ph, clampi(Y0 - P + uy, 0, pb.H - 1), clampi(X0 - P + ux, 0, pb.W - 1));
+// Up-sampled tile of TX x TY pixels with its halo, CCHUNK channels at a time, in shared memory: the vertical taps on the LR columns that
+// the tile reads, then the horizontal ones. (Sixteen taps a value, straight from memory, were a third of these kernels' instructions.)
+template <int K, int TY> struct UTile {
+    static constexpr int P = (K - 1) / 2, UW = TX + 2 * P, UH = TY + 2 * P, LC = UW + 4;      // LR columns: most at scale 1
+    float u[CCHUNK * UH * UW];
+    float v[CCHUNK * UH * LC];
+    int row0[UH], row_ph[UH], col0[UW], col_ph[UW];          // first tap of each row and column, and its phase
+    float w[kMaxScale][4];
+
+    __device__ __forceinline__ void taps(const Problem& pb, int X0, int Y0, int tid, int nthr)
+    {
+        for (int i = tid; i < UH + UW; i += nthr) {
+            const bool row = i < UH;
+            const int z = row ? clampi(Y0 - P + i, 0, pb.H - 1) : clampi(X0 - P + i - UH, 0, pb.W - 1);
+            const int q = z / pb.r, ph = z - q * pb.r;
+            if (row) { row0[i] = q + pb.ph.base[ph]; row_ph[i] = ph; }
+            else { col0[i - UH] = q + pb.ph.base[ph]; col_ph[i - UH] = ph; }
+        }
+        for (int i = tid; i < kMaxScale * 4; i += nthr) w[i / 4][i % 4] = pb.ph.w[i / 4][i % 4];
     }
-}
+    // (between barriers of the threads; taps() before)
+    __device__ __forceinline__ void fill(const float* __restrict__ lr, const Problem& pb, int f, int c0, int nc, int tid, int nthr)
+    {
+        const int lo = col0[0], nl = col0[UW - 1] + 4 - lo;
+        for (int i = tid; i < nc * UH * LC; i += nthr) {
+            const int line = i / LC, lc = i - line * LC;     // (constants)
+            if (lc < nl) {
+                const int ch = line / UH, uy = line - ch * UH;
+                const float* col = lr + ((int64_t)f * pb.c + c0 + ch) * pb.h * pb.w + clampi(lo + lc, 0, pb.w - 1);
+                const float* wy = w[row_ph[uy]];
+                float acc = 0.f;
+#pragma unroll
+                for (int a = 0; a < 4; ++a) acc = fmaf(wy[a], __ldg(col + (int64_t)clampi(row0[uy] + a, 0, pb.h - 1) * pb.w), acc);
+                v[i] = acc;
+            }
+        }
+        __syncthreads();
+        for (int i = tid; i < nc * UH * UW; i += nthr) {
+            const int line = i / UW, ux = i - line * UW;
+            const float* src = v + line * LC + col0[ux] - lo;
+            const float* wx = w[col_ph[ux]];
+            float acc = 0.f;
+#pragma unroll
+            for (int b = 0; b < 4; ++b) acc = fmaf(wx[b], src[b], acc);
+            u[i] = acc;
+        }
+    }
+};
 
 __device__ __forceinline__ void store_coef(float* p, int64_t i, float v) { p[i] = v; }
 __device__ __forceinline__ void store_coef(__half* p, int64_t i, float v) { p[i] = __float2half_rn(v); }
@@ -41,7 +77,7 @@ struct CoefGradParams {
     const float* dict;
     const float* gout;
     int mode;
-    int tiles_x, tiles_y;
+    int tiles_x, tiles_y, num_tiles;
     Problem pb;
 };
 
@@ -58,15 +94,10 @@ grad_coef_kernel(const __grid_constant__ CoefGradParams p, CoefT* __restrict__ g
     const Problem& pb = p.pb;
     const int D = pb.D, s = pb.s, H = pb.H, W = pb.W;
     float* sdict = smem;                         // [D][kkp]
-    float* sU = smem + (size_t)D * kkp;          // [CCHUNK][UH][UW]
+    UTile<K, TY>& ut = *reinterpret_cast<UTile<K, TY>*>(smem + (size_t)D * kkp);
     const int tid = threadIdx.y * TX + threadIdx.x;
     const int per = p.tiles_x * p.tiles_y;
-    const int f = blockIdx.x / per, rest = blockIdx.x - f * per;
-    const int ty = rest / p.tiles_x, tx = rest - ty * p.tiles_x;
-    const int X0 = tx * TX, Y0 = ty * TY, X = X0 + threadIdx.x, Y = Y0 + threadIdx.y;
-    const bool valid = X < W && Y < H;
     const int64_t HW = (int64_t)H * W;
-    const int64_t pix = (int64_t)min(Y, H - 1) * W + min(X, W - 1);
     const bool compact = p.mode == kModeCompact || (p.mode == kModeGlobal && (pb.flags & SR_COEF_COMPACT));
 
     for (int i = tid; i < D * kkp; i += 256) {
@@ -83,17 +114,25 @@ grad_coef_kernel(const __grid_constant__ CoefGradParams p, CoefT* __restrict__ g
             else sw[a] += g;                     // an atom listed twice counts with both weights
         }
     }
+  for (int t = blockIdx.x; t < p.num_tiles; t += gridDim.x) {
+    const int f = t / per, rest = t - f * per;
+    const int ty = rest / p.tiles_x, tx = rest - ty * p.tiles_x;
+    const int X0 = tx * TX, Y0 = ty * TY, X = X0 + threadIdx.x, Y = Y0 + threadIdx.y;
+    const bool valid = X < W && Y < H;
+    const int64_t pix = (int64_t)min(Y, H - 1) * W + min(X, W - 1);
     float G[kkp];
 #pragma unroll
     for (int j = 0; j < kkp; ++j) G[j] = 0.f;
+    __syncthreads();
+    ut.taps(pb, X0, Y0, tid, 256);
     for (int c0 = 0; c0 < pb.c; c0 += CCHUNK) {
         const int nc = min(CCHUNK, pb.c - c0);
         __syncthreads();
-        fill_u<K, TY>(p.lr, sU, pb, f, c0, nc, X0, Y0, tid, 256);
+        ut.fill(p.lr, pb, f, c0, nc, tid, 256);
         __syncthreads();
         for (int ch = 0; ch < nc; ++ch) {
             const float g = valid ? __ldg(p.gout + ((int64_t)f * pb.c + c0 + ch) * HW + pix) : 0.f;
-            const float* u = sU + ch * UH * UW + threadIdx.y * UW + threadIdx.x;
+            const float* u = ut.u + ch * UH * UW + threadIdx.y * UW + threadIdx.x;
 #pragma unroll
             for (int a = 0; a < K; ++a)
 #pragma unroll
@@ -116,10 +155,17 @@ grad_coef_kernel(const __grid_constant__ CoefGradParams p, CoefT* __restrict__ g
     const int planes = compact ? s : D;
     CoefT* out = gcoef + (int64_t)f * planes * HW + pix;
     if (p.mode == kModeCompact) {
-        for (int q = 0; q < s; ++q) {
-            const int a = min((int)__ldg(p.idx + ((int64_t)f * s + q) * HW + pix), D - 1);
-            const float v = dot(a);
-            if (valid) store_coef(out, (int64_t)q * HW, v);
+        const uint8_t* list = p.idx + (int64_t)f * s * HW + pix;
+        for (int q0 = 0; q0 < s; q0 += 8) {      // (eight loads in flight)
+            int a[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) a[i] = q0 + i < s ? min((int)__ldg(list + (int64_t)(q0 + i) * HW), D - 1) : 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (q0 + i < s) {
+                    const float v = dot(a[i]);
+                    if (valid) store_coef(out, (int64_t)(q0 + i) * HW, v);
+                }
         }
     } else if (p.mode == kModeGlobal) {
         for (int q = 0; q < planes; ++q) {
@@ -143,6 +189,7 @@ grad_coef_kernel(const __grid_constant__ CoefGradParams p, CoefT* __restrict__ g
             if (valid) store_coef(out, (int64_t)l * HW, v);
         }
     }
+  }
 }
 
 struct DictGradParams {
@@ -153,6 +200,7 @@ struct DictGradParams {
     int mode;
     int rows;                    // planes whose sums are wanted (D, or s of a subset)
     int chunk;                   // planes a block works on (gridDim.y chunks)
+    int ahead;                   // planes arrive by asynchronous copies of this many bytes (16 or 4), a tile ahead; 0 = not
     int tiles_x, tiles_y, num_tiles;
     Problem pb;
 };
@@ -176,14 +224,40 @@ grad_dict_kernel(const __grid_constant__ DictGradParams p, const CoefT* __restri
     const int rgroups = (nrow + 3) / 4, items = rgroups * TG;
     float* sG = smem;                            // [kkp][PITCH]
     float* sPhi = sG + kkp * PITCH;              // [chunk rounded up to 4][PITCH]
-    float* sU = sPhi + (size_t)((p.chunk + 3) & ~3) * PITCH;
+    const int phi = ((p.chunk + 3) & ~3) * PITCH;        // floats of a buffer of planes (two where they arrive by asynchronous copies)
+    UTile<K, TY>& ut = *reinterpret_cast<UTile<K, TY>*>(sPhi + (size_t)phi * (p.ahead ? 2 : 1));
     const int shares = max(1, 256 / items);      // threads that split the pixels of one corner
     const int share = tid / items, item = tid - share * items;
     const int rg = item / TG, tg = item - rg * TG;
     const bool works = share < shares;
 
     for (int i = tid; i < kkp * PITCH; i += 256) sG[i] = 0.f;
-    for (int i = tid; i < ((p.chunk + 3) & ~3) * PITCH; i += 256) sPhi[i] = 0.f;
+    for (int i = tid; i < phi * (p.ahead ? 2 : 1); i += 256) sPhi[i] = 0.f;
+    // A tile's planes by asynchronous copies of `ahead` bytes, a tile ahead (fp32, whole planes): 1080p x4, D = 72: 1584 -> 620 us.
+    auto fetch = [&](int t, float* to) {
+        const int per = p.tiles_x * p.tiles_y;
+        const int f = t / per, rest = t - f * per;
+        const int ty = rest / p.tiles_x, X0 = (rest - ty * p.tiles_x) * TX, Y0 = ty * TY;
+        const bool compact = (pb.flags & SR_COEF_COMPACT) != 0;
+        const int units = p.ahead == 16 ? NPX / 4 : NPX, step = p.ahead / 4;
+        for (int i = tid; i < nrow * units; i += 256) {
+            const int q = i / units, px = (i - q * units) * step, X = X0 + px % TX, Y = Y0 + px / TX;        // (units: 32 or 128)
+            int64_t plane;
+            if (p.mode == kModeGlobal) plane = compact ? (int64_t)f * s + row0 + q : (int64_t)f * D + min((int)__ldg(p.idx + row0 + q), D - 1);
+            else plane = (int64_t)f * D + row0 + q;
+            const bool in = X < W && Y < H;                              // (W a multiple of four where a copy is four pixels)
+            const CoefT* src = coef + plane * HW + (in ? (int64_t)Y * W + X : 0);
+            const uint32_t dst = (uint32_t)__cvta_generic_to_shared(to + q * PITCH + px);
+            if (step == 4) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(in ? 16 : 0) : "memory");
+            else asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(in ? 4 : 0) : "memory");
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    int buf = 0;
+    if (p.ahead) {
+        __syncthreads();
+        if ((int)blockIdx.x < p.num_tiles) fetch(blockIdx.x, sPhi);
+    }
     float total[4][4] = {};
     for (int t = blockIdx.x; t < p.num_tiles; t += gridDim.x) {
         const int per = p.tiles_x * p.tiles_y;
@@ -192,7 +266,11 @@ grad_dict_kernel(const __grid_constant__ DictGradParams p, const CoefT* __restri
         const int X0 = tx * TX, Y0 = ty * TY;
         // ---- the planes' coefficients (zero outside the image)
         __syncthreads();
-        if (p.mode == kModeIdx || p.mode == kModeCompact) {
+        const float* planes = sPhi + (p.ahead ? buf * phi : 0);
+        if (p.ahead) {
+            if (t + (int)gridDim.x < p.num_tiles) fetch(t + gridDim.x, sPhi + (buf ^ 1) * phi);
+            buf ^= 1;
+        } else if (p.mode == kModeIdx || p.mode == kModeCompact) {
             for (int i = tid; i < nrow * NPX; i += 256) sPhi[(i / NPX) * PITCH + i % NPX] = 0.f;
             __syncthreads();
             for (int i = tid; i < s * NPX; i += 256) {
@@ -218,10 +296,11 @@ grad_dict_kernel(const __grid_constant__ DictGradParams p, const CoefT* __restri
         const int px = tid % NPX, half = tid / NPX;              // two threads a pixel, every other patch row each
         const int gx = X0 + px % TX, gy = Y0 + px / TX;
         const bool valid = gx < W && gy < H;
+        ut.taps(pb, X0, Y0, tid, 256);
         for (int c0 = 0; c0 < pb.c; c0 += CCHUNK) {
             const int nc = min(CCHUNK, pb.c - c0);
             __syncthreads();
-            fill_u<K, TY>(p.lr, sU, pb, f, c0, nc, X0, Y0, tid, 256);
+            ut.fill(p.lr, pb, f, c0, nc, tid, 256);
             __syncthreads();
             float g[CCHUNK];
 #pragma unroll
@@ -233,10 +312,14 @@ grad_dict_kernel(const __grid_constant__ DictGradParams p, const CoefT* __restri
                     float v = c0 == 0 ? 0.f : sG[(a * K + b) * PITCH + px];
 #pragma unroll
                     for (int ch = 0; ch < CCHUNK; ++ch)
-                        if (ch < nc) v = fmaf(g[ch], sU[(ch * UH + px / TX + a) * UW + px % TX + b], v);
+                        if (ch < nc) v = fmaf(g[ch], ut.u[(ch * UH + px / TX + a) * UW + px % TX + b], v);
                     sG[(a * K + b) * PITCH + px] = valid ? v : 0.f;
                 }
             }
+        }
+        if (p.ahead) {                           // this tile's planes have landed; the next one's may travel on
+            if (t + (int)gridDim.x < p.num_tiles) asm volatile("cp.async.wait_group 1;" ::: "memory");
+            else asm volatile("cp.async.wait_group 0;" ::: "memory");
         }
         __syncthreads();
         // ---- the corner
@@ -245,7 +328,7 @@ grad_dict_kernel(const __grid_constant__ DictGradParams p, const CoefT* __restri
             for (int q = share; q < NPX / 4; q += shares) {
                 float4 a[4], b[4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) a[i] = *reinterpret_cast<const float4*>(sPhi + (4 * rg + i) * PITCH + 4 * q);
+                for (int i = 0; i < 4; ++i) a[i] = *reinterpret_cast<const float4*>(planes + (4 * rg + i) * PITCH + 4 * q);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) b[i] = *reinterpret_cast<const float4*>(sG + (4 * tg + i) * PITCH + 4 * q);
 #pragma unroll
@@ -354,33 +437,36 @@ grad_subset_sum_kernel(const float* __restrict__ partial, int slots, int s, int 
 
 template <typename Kern> cudaError_t raise_smem(Kern kern, size_t smem)
 {
-    return smem > 48 * 1024 ? cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) : cudaSuccess;
+    // (48 KB hold without being asked for: what is dynamic and the kernels' ten static KB)
+    return smem > 36 * 1024 ? cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) : cudaSuccess;
 }
 
 template <int K, typename CoefT> cudaError_t launch_coef_t(const GradArgs& a)
 {
-    constexpr int P = (K - 1) / 2, TY = 8;
+    constexpr int TY = 8;
     const Problem& pb = a.pb;
-    CoefGradParams p{a.lr, a.idx, a.gamma, a.dict, a.gout, a.mode, (pb.W + TX - 1) / TX, (pb.H + TY - 1) / TY, pb};
-    const int64_t blocks = (int64_t)p.tiles_x * p.tiles_y * pb.n;
-    if (blocks > 0x7FFFFFFF) return cudaErrorInvalidConfiguration;
-    const size_t smem = ((size_t)pb.D * KK<K>::padded + (size_t)CCHUNK * (TY + 2 * P) * (TX + 2 * P)) * sizeof(float);
+    CoefGradParams p{a.lr, a.idx, a.gamma, a.dict, a.gout, a.mode, (pb.W + TX - 1) / TX, (pb.H + TY - 1) / TY, 0, pb};
+    const int64_t tiles = (int64_t)p.tiles_x * p.tiles_y * pb.n;
+    if (tiles > 0x7FFFFFFF) return cudaErrorInvalidConfiguration;
+    p.num_tiles = (int)tiles;
+    const int blocks = (int)(tiles < 4 * sm_count() ? tiles : 4 * sm_count());
+    const size_t smem = (size_t)pb.D * KK<K>::padded * sizeof(float) + sizeof(UTile<K, TY>);
     auto kern = grad_coef_kernel<K, CoefT>;
     if (cudaError_t e = raise_smem(kern, smem)) return e;
-    kern<<<(unsigned)blocks, dim3(TX, TY), smem, a.st>>>(p, static_cast<CoefT*>(a.gcoef));
+    kern<<<blocks, dim3(TX, TY), smem, a.st>>>(p, static_cast<CoefT*>(a.gcoef));
     count_launches(1);
     return cudaGetLastError();
 }
 
 template <int K, typename CoefT> cudaError_t launch_dict_t(const GradArgs& a, int* slots)
 {
-    constexpr int P = (K - 1) / 2, TY = 4, TG = KK<K>::padded / 4, PITCH = TX * TY + 4;
+    constexpr int TY = 4, TG = KK<K>::padded / 4, PITCH = TX * TY + 4;
     const Problem& pb = a.pb;
     DictGradParams p{};
     p.lr = a.lr; p.idx = a.idx; p.gout = a.gout; p.partial = a.scratch; p.mode = a.mode; p.pb = pb;
     p.rows = grad_rows(a);
-    // planes of a block: at most 256 corners of 4 x 4, and 128 planes (shared memory)
-    constexpr int kMost = 4 * (256 / TG) < 128 ? 4 * (256 / TG) : 128;
+    // planes of a block: at most 256 corners of 4 x 4, and 80 planes (shared memory)
+    constexpr int kMost = 4 * (256 / TG) < 80 ? 4 * (256 / TG) : 80;
     const int chunks = (p.rows + kMost - 1) / kMost;
     p.chunk = ((p.rows + chunks - 1) / chunks + 3) & ~3;
     p.tiles_x = (pb.W + TX - 1) / TX;
@@ -389,7 +475,9 @@ template <int K, typename CoefT> cudaError_t launch_dict_t(const GradArgs& a, in
     if (tiles > 0x7FFFFFFF) return cudaErrorInvalidConfiguration;
     p.num_tiles = (int)tiles;
     const int gx = (int)(tiles < grad_slots() ? tiles : grad_slots());
-    size_t smem = ((size_t)(KK<K>::padded + p.chunk) * PITCH + (size_t)CCHUNK * (TY + 2 * P) * (TX + 2 * P)) * sizeof(float);
+    const bool whole = a.mode == kModeDense || a.mode == kModeGlobal;
+    p.ahead = sizeof(CoefT) == 4 && whole ? (pb.W % 4 == 0 && ((uintptr_t)a.coef & 15) == 0 ? 16 : 4) : 0;
+    size_t smem = ((size_t)KK<K>::padded + (size_t)p.chunk * (p.ahead ? 2 : 1)) * PITCH * sizeof(float) + sizeof(UTile<K, TY>);
     const size_t sums = (size_t)((p.chunk + 3) / 4) * TG * 16 * sizeof(float);
     if (smem < sums) smem = sums;
     auto kern = grad_dict_kernel<K, CoefT>;

@@ -580,6 +580,12 @@ template <int K> bool plan_fits(const GradArgs& a)
 bool grad_roles_supported(const GradArgs& a)
 {
     if (!form_supported(a) || a.pb.D > 128) return false;
+    // Two load warps without asynchronous copies do not keep up with whole planes (odd widths: 1077 x 1080, D = 72: both gradients 686 us,
+    // 537 by the two kernels of sr_grad_tc.cu), nor with the dictionary's sums over lists alone (1080p x4, s = 8: 473 / 303; both
+    // gradients 545 / 768).
+    const bool sums = a.gdict || a.ggamma;
+    if (sums && (a.mode == kModeDense || a.mode == kModeGlobal) && (a.pb.W % 2 != 0 || ((uintptr_t)a.coef & 3) != 0)) return false;
+    if (sums && !a.gcoef && (a.mode == kModeIdx || a.mode == kModeCompact)) return false;
     switch (a.pb.k) {
     case 3: return plan_fits<3>(a);
     case 5: return plan_fits<5>(a);

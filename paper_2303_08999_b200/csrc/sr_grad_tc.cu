@@ -302,12 +302,20 @@ grad_dict_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_consta
             const int64_t pix = (int64_t)(w.y0 + row) * W + w.x0 + x;
             if (!p.tma && ok) {
                 if (p.mode == kModeIdx || p.mode == kModeCompact) {
-                    // the atoms that the pixel listed a row ago are cleared by the thread that wrote them (below)
-                    if (inside)
-                        for (int q = 0; q < s_; ++q) {
-                            const int a = min((int)__ldg(p.idx + ((int64_t)w.f * s_ + q) * HW + pix), D - 1);
-                            *place(a) = __ldg(p.coef + (p.mode == kModeCompact ? (int64_t)w.f * s_ + q : (int64_t)w.f * D + a) * HW + pix);
-                        }
+                    // (what a row put there is taken back by the thread that did, below)
+                    const uint8_t* list = p.idx + (int64_t)w.f * s_ * HW + pix;
+                    const __half* src = p.coef + (int64_t)w.f * p.planes * HW + pix;
+                    for (int q0 = 0; inside && q0 < s_; q0 += 8) {       // (eight loads in flight: one after the other took 250 us at 1080p, s = 8)
+                        int a[8];
+                        __half h[8];
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) a[i] = q0 + i < s_ ? min((int)__ldg(list + (int64_t)(q0 + i) * HW), D - 1) : 0;
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) h[i] = q0 + i < s_ ? __ldg(src + (int64_t)(p.mode == kModeCompact ? q0 + i : a[i]) * HW) : __ushort_as_half(0);
+#pragma unroll
+                        for (int i = 0; i < 8; ++i)
+                            if (q0 + i < s_) *place(a[i]) = h[i];
+                    }
                 } else {
                     const bool gather = p.mode == kModeGlobal && !(pb.flags & SR_COEF_COMPACT);
                     const __half* src = p.coef + (int64_t)w.f * p.planes * HW + pix;
@@ -350,9 +358,15 @@ grad_dict_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_consta
                 ok = __all_sync(0xffffffffu, mbar_wait_short(&ctl.mma[grp], phase, wc));
                 phase ^= 1;
                 in_work = false;
-                if (inside && ok)
-                    for (int q = 0; q < s_; ++q)
-                        *place(min((int)__ldg(p.idx + ((int64_t)w.f * s_ + q) * HW + pix), D - 1)) = __ushort_as_half(0);
+                const uint8_t* list = p.idx + (int64_t)w.f * s_ * HW + pix;
+                for (int q0 = 0; inside && ok && q0 < s_; q0 += 8) {
+                    int a[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) a[i] = q0 + i < s_ ? min((int)__ldg(list + (int64_t)(q0 + i) * HW), D - 1) : -1;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        if (a[i] >= 0) *place(a[i]) = __ushort_as_half(0);
+                }
             }
         }
         if (!ok) continue;                       // (the next tile's barrier, or the end, tells the block)
