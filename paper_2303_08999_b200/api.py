@@ -417,21 +417,22 @@ def sr_tune_reset() -> None:
     load_library().sr_tune_reset()
 
 
-def _scratch(nbytes: int, scratch, device, what: str) -> torch.Tensor:
-    """`scratch` checked, or a new buffer of nbytes on `device`."""
+def _scratch(nbytes: int, scratch, like, what: str) -> torch.Tensor:
+    """`scratch` checked, or a new buffer of nbytes on like's device."""
     if nbytes == 0:
         raise SrError(SR_ERR_UNSUPPORTED, what)
     if scratch is None:
-        return torch.empty(nbytes, dtype=torch.uint8, device=device)
+        return like.new_empty(nbytes, dtype=torch.uint8)
     return _dev(scratch, torch.uint8, "scratch")
 
 
 def _same_device(first, **others):
     """All tensors on the current device, whose stream the call runs on."""
-    if _get_device is not None and first.get_device() != _get_device():
+    at = first.get_device()
+    if _get_device is not None and at != _get_device():
         raise ValueError(f"the tensors are on {first.device}, the current device is cuda:{_get_device()}")
     for what, t in others.items():
-        if t is not None and t.device != first.device:
+        if t is not None and t.get_device() != at:
             raise ValueError(f"{what} is on {t.device}, lr or coef on {first.device}")
 
 
@@ -440,9 +441,9 @@ def _grad_out_of(t, shape, dtype, want: bool, like, what: str):
     if not want:
         return None
     if t is None:
-        return torch.empty(shape, dtype=dtype, device=like.device)
+        return like.new_empty(shape, dtype=dtype)
     _dev(t, dtype, what)
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         raise ValueError(f"{what} must be {tuple(shape)}")
     return t
 
@@ -465,7 +466,7 @@ def sr_dict_regress_dense_grad(lr, coef, dict_, grad_out, scale: int, k: int, fl
     d = sr_dims(n, c, h, w, scale, k, D)
     lib = _lib or load_library()
     if want_dict:
-        scratch = _scratch(lib.sr_dict_regress_grad_scratch_bytes(ctypes.byref(d)), scratch, lr.device, "sr_dict_regress_grad_scratch_bytes")
+        scratch = _scratch(lib.sr_dict_regress_grad_scratch_bytes(ctypes.byref(d)), scratch, lr, "sr_dict_regress_grad_scratch_bytes")
     status = lib.sr_dict_regress_dense_grad(lr.data_ptr(), coef.data_ptr(), code, dict_.data_ptr(), grad_out.data_ptr(), _ptr(grad_coef),
                                             _ptr(grad_dict), ctypes.byref(d), flags, _ptr(scratch), 0 if scratch is None else scratch.numel(), _stream())
     if status:
@@ -501,7 +502,7 @@ def sr_dict_regress_selected_grad(lr, coef_or_sel, idx, gamma, dict_, grad_out, 
     d = sr_dims(n, c, h, w, scale, k, D)
     lib = _lib or load_library()
     if want_dict:
-        scratch = _scratch(lib.sr_dict_regress_grad_scratch_bytes(ctypes.byref(d)), scratch, lr.device, "sr_dict_regress_grad_scratch_bytes")
+        scratch = _scratch(lib.sr_dict_regress_grad_scratch_bytes(ctypes.byref(d)), scratch, lr, "sr_dict_regress_grad_scratch_bytes")
     status = lib.sr_dict_regress_selected_grad(lr.data_ptr(), coef_or_sel.data_ptr(), code, idx.data_ptr(), _ptr(gamma), dict_.data_ptr(),
                                                grad_out.data_ptr(), _ptr(grad_coef), _ptr(grad_dict), _ptr(grad_gamma), ctypes.byref(d), s, flags,
                                                _ptr(scratch), 0 if scratch is None else scratch.numel(), _stream())
@@ -522,10 +523,9 @@ def sr_select_balance(coef, idx, mask=None, flags: int = 0, scratch=None):
     _same_device(coef, idx=idx, mask=mask, scratch=scratch)
     d = sr_dims(n, 1, H, W, 1, 1, D)
     lib = _lib or load_library()
-    scratch = _scratch(lib.sr_select_balance_scratch_bytes(ctypes.byref(d)), scratch, coef.device, "sr_select_balance_scratch_bytes")
-    loss = torch.empty(1, dtype=torch.float32, device=coef.device)
-    counts = torch.empty((n, D), dtype=torch.int32, device=coef.device)
-    share, slope = torch.empty((2, n, D), dtype=torch.float32, device=coef.device)
+    scratch = _scratch(lib.sr_select_balance_scratch_bytes(ctypes.byref(d)), scratch, coef, "sr_select_balance_scratch_bytes")
+    loss, counts = coef.new_empty(1, dtype=torch.float32), coef.new_empty((n, D), dtype=torch.int32)
+    share, slope = coef.new_empty((n, D), dtype=torch.float32), coef.new_empty((n, D), dtype=torch.float32)
     status = lib.sr_select_balance(coef.data_ptr(), code, idx.data_ptr(), _ptr(mask), loss.data_ptr(), counts.data_ptr(), share.data_ptr(),
                                    slope.data_ptr(), ctypes.byref(d), s, flags, scratch.data_ptr(), scratch.numel(), _stream())
     if status:

@@ -73,7 +73,7 @@ cudaError_t launch_adamw(const sr_adamw_tensor* tensors, int count, int param_dt
 // A kernel that sums what the launch before it on the stream wrote: it may be brought up while that one ends (programmatic dependent
 // launch) and waits for its end, with all it wrote, in wait_for_launch_before().
 template <typename... Params, typename... Args>
-cudaError_t launch_after(void (*kern)(Params...), dim3 grid, int threads, cudaStream_t st, Args... args)
+cudaError_t launch_after_smem(void (*kern)(Params...), dim3 grid, int threads, size_t smem, cudaStream_t st, Args... args)
 {
     cudaLaunchAttribute attr{};
     attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -81,11 +81,20 @@ cudaError_t launch_after(void (*kern)(Params...), dim3 grid, int threads, cudaSt
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = grid;
     cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
     return cudaLaunchKernelEx(&cfg, kern, static_cast<Params>(args)...);
 }
+template <typename... Params, typename... Args>
+cudaError_t launch_after(void (*kern)(Params...), dim3 grid, int threads, cudaStream_t st, Args... args)
+{
+    return launch_after_smem(kern, grid, threads, 0, st, args...);
+}
+
+// In the launch before: the next one may be brought up now, beside this one (one that depends on nothing this one writes).
+__device__ __forceinline__ void let_next_launch_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void wait_for_launch_before() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 #endif
 
