@@ -289,6 +289,110 @@ def test_streams_and_graph_replay(mode):
     assert sr.sr_device_status() == 0
 
 
+@pytest.mark.parametrize("w", [632, 636, 634, 633])          # TMA, copies of 8 and 4 bytes, single elements
+@pytest.mark.parametrize("k,D,c", [(3, 16, 3), (5, 72, 3), (7, 40, 1), (5, 128, 4), (7, 128, 3), (5, 200, 3)])
+@pytest.mark.parametrize("mode", ["dense", "listed", "compact", "global", "global compact"])
+def test_frames_of_many_tiles_a_block(w, k, D, c, mode):
+    """Every ring of the pipelines wraps many times: 1.2 million pixels, every element of both gradients against fp64 on the device."""
+    n, h, s, compact = 3, 640, 6, mode.endswith("compact")
+    gen = torch.Generator(device="cuda").manual_seed(D + k + w)
+    lr = torch.rand((n, c, h, w), device="cuda", generator=gen)
+    coef = torch.empty((n, D, h, w), device="cuda", dtype=torch.float16).normal_(1 / D, 0.05, generator=gen)
+    g = torch.empty((n, c, h, w), device="cuda").normal_(0, 0.05, generator=gen)
+    d = torch.empty((D, k * k), device="cuda").normal_(0, 0.2, generator=gen)
+    idx = gamma = None
+    flags = sr.SR_COEF_COMPACT if compact else 0
+    if mode in ("listed", "compact"):
+        idx = sr.sr_dict_select(coef, s)
+        coef = torch.gather(coef, 1, idx.long()).contiguous() if compact else coef
+    elif mode != "dense":
+        idx = torch.randperm(D, device="cuda", generator=gen)[:s].to(torch.uint8)
+        gamma = torch.empty(s, device="cuda").uniform_(0.5, 1.5, generator=gen)
+        coef, flags = coef[:, idx.long()].contiguous() if compact else coef, flags | sr.SR_IDX_GLOBAL
+    if mode == "dense":
+        gc, gd = sr.sr_dict_regress_dense_grad(lr, coef, d, g, 1, k)
+        again = sr.sr_dict_regress_dense_grad(lr, coef, d, g, 1, k)
+        alone = (sr.sr_dict_regress_dense_grad(lr, coef, d, g, 1, k, want_dict=False)[0], sr.sr_dict_regress_dense_grad(lr, coef, d, g, 1, k, want_coef=False)[1])
+    else:
+        call = lambda **kw: sr.sr_dict_regress_selected_grad(lr, coef, idx, gamma, d, g, 1, k, s, flags, **kw)  # noqa: E731
+        gc, gd, gg = call()
+        again, alone = call(), (call(want_dict=False)[0], call(want_coef=False)[1])
+    assert sr.sr_device_status() == 0
+    assert torch.equal(gc, again[0]) and torch.equal(gd, again[1])                   # the same bits on every run
+    p, atoms = (k - 1) // 2, d.double()
+    if gamma is not None:
+        atoms = d[idx.long()].double() * gamma.double().view(-1, 1)
+    A, worst, magnitude = torch.zeros_like(atoms), [0.0, 0.0], 0.0
+    for f in range(n):                                                               # scale 1: the image itself
+        pad = torch.nn.functional.pad(lr[f:f + 1].double(), (p, p, p, p), mode="replicate")[0]
+        G = torch.stack([(pad[:, a:a + h, b:b + w] * g[f].double()).sum(0) for a in range(k) for b in range(k)], -1)
+        full = torch.einsum("hwj,lj->lhw", G, atoms)
+        bound = torch.einsum("hwj,lj->lhw", G.abs(), atoms.abs())
+        weights = coef[f].double()
+        if mode == "listed":
+            keep = torch.zeros_like(weights).scatter_(0, idx[f].long(), 1.0)
+            full, weights = full * keep, weights * keep
+        elif mode == "compact":
+            weights = torch.zeros((D, h, w), dtype=torch.float64, device="cuda").scatter_(0, idx[f].long(), weights)
+            full, bound = torch.gather(full, 0, idx[f].long()), torch.gather(bound, 0, idx[f].long())
+        elif mode == "global":
+            at = idx.long()
+            weights = weights[at]
+            spread = torch.zeros((D, h, w), dtype=torch.float64, device="cuda")
+            full, bound = spread.index_copy(0, at, full), spread.index_copy(0, at, bound)
+        for i, got in enumerate((gc, alone[0])):                                     # |.| of the terms bounds every rounding (see the top of this file)
+            worst[i] = max(worst[i], float(((got[f].double() - full).abs() / (full.abs() * U16 + (2 * (k * k + c + 16) + 16) * 2 * U32 * bound + 2.0 ** -25)).max()))
+        A += torch.einsum("lhw,hwj->lj", weights, G)
+        magnitude = magnitude + torch.einsum("lhw,hwj->lj", weights.abs(), G.abs())
+    assert worst[0] <= 1.0 and worst[1] <= 1.0, worst
+    want = A
+    if gamma is not None:
+        want = torch.zeros((D, k * k), dtype=torch.float64, device="cuda").index_copy(0, idx.long(), A * gamma.double().view(-1, 1))
+        assert float((gg.double() - (d[idx.long()].double() * A).sum(1)).norm()) <= 2e-6 * float((d[idx.long()].double().abs() * magnitude).sum(1).norm())
+    for got in (gd, alone[1]):
+        assert float((got.double() - want).norm()) <= 2e-6 * float(magnitude.norm())
+
+
+@pytest.mark.parametrize("case", ["dense", "listed", "more atoms", "odd width"])
+def test_a_wait_that_runs_out_is_reported_and_the_next_call_is_clean(case):
+    """One product's completion is never announced (the hook of the forward calls): the block gives up, nothing hangs, the status says so."""
+    D, w = (160, 64) if case == "more atoms" else (40, 33 if case == "odd width" else 64)
+    lr, coef, d, g = (to(a) for a in _inputs(1, 3, 24, w, 1 if case == "odd width" else 2, D, 5, "f16", seed=13))
+    r = 1 if case == "odd width" else 2
+    idx = sr.sr_dict_select(coef, 4) if case == "listed" else None
+
+    def call():
+        if idx is not None:
+            return sr.sr_dict_regress_selected_grad(lr, coef, idx, None, d, g, r, 5, 4)[:2]
+        return sr.sr_dict_regress_dense_grad(lr, coef, d, g, r, 5)
+    before = [t.clone() for t in call()]
+    assert sr.sr_device_status() == 0
+    old = sr.sr_set_wait_limit(2_000_000)
+    try:
+        sr.sr_test_lose_arrival(1)
+        call()
+        assert sr.sr_device_status() == 6 and sr.sr_device_status() == 0             # SR_ERR_TIMEOUT, once
+    finally:
+        sr.sr_test_lose_arrival(0)
+        sr.sr_set_wait_limit(old)
+    assert all(torch.equal(a, b) for a, b in zip(call(), before)) and sr.sr_device_status() == 0
+
+
+def test_two_calls_at_once_with_a_scratch_each():
+    data = [tuple(to(a) for a in _inputs(2, 3, 60, 80, 4, 72, 5, "f16", seed=40 + i)) for i in range(2)]
+    want = [[t.clone() for t in sr.sr_dict_regress_dense_grad(*x, 4, 5)] for x in data]
+    streams = [torch.cuda.Stream() for _ in data]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(5):
+        for i, (st, x) in enumerate(zip(streams, data)):
+            with torch.cuda.stream(st):
+                got[i].append(sr.sr_dict_regress_dense_grad(*x, 4, 5))
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for i in (0, 1) for run in got[i] for a, b in zip(run, want[i]))
+    assert sr.sr_device_status() == 0
+
+
 def test_full_size_frames_on_sampled_pixels_and_every_atom():
     """The headline frame and a batch whose element offsets pass 2^31: grad_coef at pixels on both sides of the tiles' seams, all of
     grad_dict, against fp64 on the device."""
