@@ -35,6 +35,10 @@ static_assert(kRegsLaunch * kRoleThreads <= 65536, "the launch's registers fit t
 static_assert(kFG * 128 * kRegsG + kRG * 128 * kRegsResult + 128 * kRegsLoad <= kRegsLaunch * kRoleThreads, "the roles' registers are the launch's");
 constexpr int kRoleReserve = 6656;                           // static shared memory, kept out of the dynamic budget
 constexpr int kMaxG = 4, kMaxP = 4, kUnscales = 16;
+// Rows whose dictionary sums stay in tensor memory: its additions cut off, so every one shrinks the sum by a third of 2^-24 (8 rows, 64
+// additions: 1.1e-6 too small; 4 rows: half of that). Segment m of the block is accumulated in buffer m & 1 and taken by that result group.
+constexpr int kSegment = 4;
+__device__ __forceinline__ int segments(int rows) { return (rows + kSegment - 1) / kSegment; }
 // G tiles (those of 7 x 7 are twice as large). At least as many as groups: a group that waits for a tile's use u must know that use u - 2
 // is over (a barrier tells only the parity of its phase); its own row before, kFG rows back, waited for the row kRing before that one.
 template <int K> constexpr int kRing = K == 7 ? 2 : kMaxG;
@@ -247,13 +251,13 @@ template <int K, bool COEF> __device__ __forceinline__ void mma_role(const RoleP
     constexpr uint32_t idesc = COEF ? make_idesc_f16(128, 128, false, false) : make_idesc_f16(128, G::NB, false, true);
     bool lose = p.b.lose != 0 && blockIdx.x == 0 && (COEF || !p.want_coef);
     bool ok = true;
-    int gs = 0, ps = 0;                                      // ring entries of the row
+    int gs = 0, ps = 0, seg = 0;                             // ring entries of the row; segment
     uint32_t gp = 0, pp = 0;                                 // and the parities of their uses
     for (Tiles tl(p.b.g); tl.more(p.b.g) && ok; tl.next(p.b.g)) {
         for (int row = 0; row < tl.rows; ++row) {
             const int item = tl.base + row;
             if (COEF) ok = wait_all(&ctl.c_empty[item & 1], ((item >> 1) & 1) ^ 1, wc, ok);
-            else if (row == 0) ok = wait_all(&ctl.d_empty[tl.n & 1], ((tl.n >> 1) & 1) ^ 1, wc, ok);
+            else if (row % kSegment == 0) ok = wait_all(&ctl.d_empty[seg & 1], ((seg >> 1) & 1) ^ 1, wc, ok);
             if (!COEF) ok = wait_all(&ctl.p_full[ps], pp, wc, ok);
             ok = wait_all(&ctl.g_full[gs], gp, wc, ok);
             if (!ok) break;
@@ -271,18 +275,19 @@ template <int K, bool COEF> __device__ __forceinline__ void mma_role(const RoleP
                     }
                     if (!lose) mma_commit(&ctl.c_full[item & 1]);
                 } else {
-                    const uint32_t acc = tmem + 256 + (tl.n & 1) * G::NB;
+                    const uint32_t acc = tmem + 256 + (seg & 1) * G::NB;
                     const uint64_t ad = a_desc0 + ((uint32_t)(ps * p.b.stage_bytes) >> 4);
 #pragma unroll
                     for (int ks = 0; ks < 8; ++ks)
-                        mma_f16_ss(acc, ad + (ks >> 2) * a_chunk + (ks & 3) * 2, gd + (uint32_t)(ks * 2048 >> 4), idesc, row > 0 || ks > 0);
+                        mma_f16_ss(acc, ad + (ks >> 2) * a_chunk + (ks & 3) * 2, gd + (uint32_t)(ks * 2048 >> 4), idesc, row % kSegment > 0 || ks > 0);
                     if (!lose) mma_commit(&ctl.p_empty[ps]);
-                    if (row == tl.rows - 1) mma_commit(&ctl.d_full[tl.n & 1]);
+                    if (row % kSegment == kSegment - 1 || row == tl.rows - 1) mma_commit(&ctl.d_full[seg & 1]);
                 }
                 mma_commit(&ctl.g_empty[gs]);
             }
             __syncwarp();
             lose = false;
+            if (row % kSegment == kSegment - 1 || row == tl.rows - 1) ++seg;
             if (++gs == kRing<K>) { gs = 0; gp ^= 1; }
             if (++ps == p.p_stages) { ps = 0; pp ^= 1; }
         }
@@ -321,6 +326,7 @@ template <int K, bool FAST> __device__ __forceinline__ void result_role(const CU
     uint8_t* chunk = s.out + grp * kOutBytes;                // 64 pixels of the group's 128 atoms
     uint8_t* to = chunk + warp * 4096;
     bool ok = true;
+    int seg = 0;
     for (Tiles tl(p.b.g); tl.more(p.b.g) && ok; tl.next(p.b.g)) {
         for (int row = (tl.base + grp) & 1; p.want_coef && row < tl.rows; row += kRG) {      // rows whose number is grp modulo 2
             const int item = tl.base + row;
@@ -434,14 +440,15 @@ template <int K, bool FAST> __device__ __forceinline__ void result_role(const CU
             }
             if (!ok) break;
         }
-        if (p.want_dict && grp == 0 && ok) {
-            ok = wait_all(&ctl.d_full[tl.n & 1], (tl.n >> 1) & 1, wc, ok);
+        for (const int stop = seg + segments(tl.rows); seg < stop && p.want_dict && ok; ++seg) {
+            if ((seg & 1) != grp) continue;
+            ok = wait_all(&ctl.d_full[grp], (seg >> 1) & 1, wc, ok);
             if (together) ok = result_barrier(ok);
             tc_fence_after_sync();
             if (!ok) break;
             const float un = *(volatile float*)&ctl.unscale[tl.n % kUnscales];
             if (32 * warp < p.b.rows) {
-                const uint32_t d = at + 256 + (tl.n & 1) * G::NB;
+                const uint32_t d = at + 256 + grp * G::NB;
 #pragma unroll
                 for (int j0 = 0; j0 < G::kk; j0 += 16) {
                     float hi[16], lo[16];
@@ -455,14 +462,25 @@ template <int K, bool FAST> __device__ __forceinline__ void result_role(const CU
             }
             tc_fence_before_sync();
             __syncwarp();
-            if (lane == 0) mbar_arrive(&ctl.d_empty[tl.n & 1]);
+            if (lane == 0) mbar_arrive(&ctl.d_empty[grp]);
         }
     }
     if (lane == 0) bulk_wait_all();
-    if (p.want_dict && grp == 0 && l < p.b.rows) {
-        float* out = p.b.partial + ((int64_t)blockIdx.x * p.b.rows + l) * G::kk;
+    // the groups' sums added in their order, through shared memory that every role has left by now
+    tc_fence_before_sync();
+    __syncthreads();                                         // (the block's last barrier: the other roles' is in the kernel)
+    if (p.want_dict) {
+        float* sum = reinterpret_cast<float*>(s.G);          // (49 x 128 floats at most, less than a ring)
+        if (grp == 1 && l < p.b.rows) {
 #pragma unroll
-        for (int j = 0; j < G::kk; ++j) out[j] = total[j];
+            for (int j = 0; j < G::kk; ++j) sum[j * 128 + l] = total[j];
+        }
+        asm volatile("barrier.cta.sync 4, %0;" ::"n"(kRG * kGroupThreads) : "memory");
+        if (grp == 0 && l < p.b.rows) {
+            float* out = p.b.partial + ((int64_t)blockIdx.x * p.b.rows + l) * G::kk;
+#pragma unroll
+            for (int j = 0; j < G::kk; ++j) out[j] = total[j] + sum[j * 128 + l];
+        }
     }
 }
 
@@ -516,10 +534,12 @@ grad_roles_kernel(const __grid_constant__ CUtensorMap map_in, const __grid_const
         else if (p.want_dict) load_role<FAST>(&map_in, p, ctl, s.Phi, tid - kLoadWarp * 32);
     }
 
-    __syncwarp();
-    tc_fence_before_sync();
-    __syncthreads();
-    tc_fence_after_sync();
+    if (warp < kResultWarp || warp >= kLoadWarp) {
+        __syncwarp();
+        tc_fence_before_sync();
+        __syncthreads();                                     // (the result warps': in their role)
+        tc_fence_after_sync();
+    }
     if (ctl.c.wait.abort_flag && tid == 0) atomicExch(p.b.status, SR_ERR_TIMEOUT);
     if (warp == kMmaWarp) tmem_dealloc(tmem, 512);
 }
