@@ -5,8 +5,9 @@
 // (1080p x4, D = 72, k = 5: 129 + 129 us in two kernels, 34 of each the up-sampled tile, against 95 us of traffic). Here one block per
 // multiprocessor holds a pipeline, and G, which costs most, is computed once for both products:
 //   G warps (kFG groups of four)   the up-sampled tile; G of every row, hi + lo, into a ring of tiles         g_full
-//   load warps (two)               the row's coefficients into a ring of stages: TMA boxes, or (widths and    p_full
-//                                  addresses TMA does not take, gathered planes, lists) a pixel a thread
+//   load warps (two; lists: six)   the row's coefficients into a ring of stages: TMA boxes (lists: masked      p_full
+//                                  there), or (widths and addresses TMA does not take, gathered planes,
+//                                  compact values) smaller asynchronous copies or a pixel a thread
 //   MMA warps (one a product)      a row's coefficient gradients in one of two accumulators (lane = atom,     c_full, g_empty
 //                                  column = pixel), the dictionary's sums over the tile in one of two more     d_full, p_empty, g_empty
 //   result warps (kRG groups of four)  a row's coefficient gradients to memory (c_empty), the tile's dictionary sums to registers (d_empty)
@@ -25,14 +26,24 @@ using namespace gradtc;
 
 constexpr int kFG = 2;                                       // groups of G warps
 constexpr int kRG = 2;                                       // groups of result warps: rows of one accumulator each
-constexpr int kResultWarp = kFG * 4, kLoadWarp = kResultWarp + kRG * 4, kMmaWarp = kLoadWarp + 2;
-constexpr int kRoleThreads = (kMmaWarp + 2) * 32, kLoadThreads = 64;
+// What a kernel is compiled for. kFast: results by TMA, coefficients by TMA or asynchronous copies; without the other ways' code its roles
+// keep their values in registers (1080p x4: 188 -> 162 us). kLists: lists, both by TMA. kGeneral: the rest.
+enum Form { kGeneral, kFast, kLists };
+constexpr int kResultWarp = kFG * 4, kLoadWarp = kResultWarp + kRG * 4, kLoadThreads = 64;
+constexpr int kListPairs = 3;                                // pairs of load warps of kLists: a row a pair, in turn
+template <Form F> constexpr int kMmaWarp = kLoadWarp + (F == kLists ? 2 * kListPairs : 2);
+template <Form F> constexpr int kRoleThreads = (kMmaWarp<F> + 2) * 32;
 // Registers a thread: of the launch, and after the G warps have taken what the others do not need (whole warpgroups; an increase beyond
 // what the block was launched with would wait for ever).
-constexpr int kRegsLaunch = 96, kRegsG = 112, kRegsResult = 104, kRegsLoad = 48;
-static_assert(kRegsG >= kRegsLaunch && kRegsResult >= kRegsLaunch && kRegsLoad <= kRegsLaunch, "inc, inc and dec below (the other direction is an illegal instruction)");
-static_assert(kRegsLaunch * kRoleThreads <= 65536, "the launch's registers fit the multiprocessor");
-static_assert(kFG * 128 * kRegsG + kRG * 128 * kRegsResult + 128 * kRegsLoad <= kRegsLaunch * kRoleThreads, "the roles' registers are the launch's");
+template <Form F> constexpr int kRegsLaunch = F == kLists ? 80 : 96;
+template <Form F> constexpr int kRegsG = F == kLists ? 104 : 112;
+template <Form F> constexpr int kRegsResult = F == kLists ? 88 : 104;
+constexpr int kRegsLoad = 48;
+template <Form F> constexpr bool kRegsFit =
+    kRegsG<F> >= kRegsLaunch<F> && kRegsResult<F> >= kRegsLaunch<F> && kRegsLoad <= kRegsLaunch<F> &&   // inc, inc, dec: the other direction is illegal
+    kRoleThreads<F> % 128 == 0 && kRegsLaunch<F> * kRoleThreads<F> <= 65536 &&
+    128 * (kFG * kRegsG<F> + kRG * kRegsResult<F> + (kRoleThreads<F> / 128 - kFG - kRG) * kRegsLoad) <= kRegsLaunch<F> * kRoleThreads<F>;
+static_assert(kRegsFit<kGeneral> && kRegsFit<kFast> && kRegsFit<kLists>, "the roles' registers are the launch's");
 constexpr int kRoleReserve = 6656;                           // static shared memory, kept out of the dynamic budget
 constexpr int kMaxG = 4, kMaxP = 4, kUnscales = 16;
 // Rows whose dictionary sums stay in tensor memory: its additions cut off, so every one shrinks the sum by a third of 2^-24 (8 rows, 64
@@ -42,12 +53,17 @@ __device__ __forceinline__ int segments(int rows) { return (rows + kSegment - 1)
 // G tiles (those of 7 x 7 are twice as large). At least as many as groups: a group that waits for a tile's use u must know that use u - 2
 // is over (a barrier tells only the parity of its phase); its own row before, kFG rows back, waited for the row kRing before that one.
 template <int K> constexpr int kRing = K == 7 ? 2 : kMaxG;
+// Lists: rows of bits, one for each of a row's pixels and 128 atoms. Every stage has one pair of load warps, and every entry of bits one pair
+// and one result group (two entries a pair), for the same reason: a wait for the use before follows that warp's own use before.
+constexpr int kBitsRing = 2 * kListPairs, kBitsBytes = 128 * 16;
+static_assert(kRG == 2, "two entries a pair");
 static_assert(kRing<7> >= kFG && kRing<5> >= kFG, "a group is never two uses ahead of a ring entry");
 
 struct __align__(16) RoleCtl {
-    GradCtl c;                                               // (its mma / full barriers are not used)
+    GradCtl c;
     uint64_t g_full[kMaxG], g_empty[kMaxG], p_full[kMaxP], p_empty[kMaxP];
     uint64_t c_full[2], c_empty[2], d_full[2], d_empty[2];
+    uint64_t p_land[kMaxP], b_full[kBitsRing], b_empty[kBitsRing];
     float unscale[kUnscales];                                // of the tiles, by number
     float back[128];                                         // 2^e of each plane's atom (0: a plane outside the subset)
     uint32_t listed[kRG][128][4];                            // lists: the pixels of a group's row that list the atom
@@ -63,20 +79,23 @@ struct RoleParams {
     int out_pairs;               // results stored two pixels at a time (where not by TMA)
     int copy_bytes;              // coefficients by asynchronous copies of this size; 0 = TMA or one by one
     int want_coef, want_dict;
+    int lists;                   // lists over planes that TMA takes: pairs of load warps that mask them, and make the bits for the result warps;
+                                 // as many as stages
 };
 
 template <int K> struct RoleSmem {
-    uint8_t *G, *D, *out, *Phi;
+    uint8_t *G, *D, *out, *bits, *Phi;
     Floats f;
 };
-// [G ring][atoms][results][coefficient ring][floats]
+// [G ring][atoms][results][bits][coefficient ring][floats]
 template <int K> __device__ __forceinline__ RoleSmem<K> carve(uint8_t* at, const RoleParams& p)
 {
     RoleSmem<K> s;
     s.G = at;
     s.D = s.G + kRing<K> * GGeo<K>::G_BYTES;
     s.out = s.D + (p.want_coef ? GGeo<K>::BLOCKS * p.d_block : 0);
-    s.Phi = s.out + (p.want_coef ? kRG * kOutBytes : 0);
+    s.bits = s.out + (p.want_coef ? kRG * kOutBytes : 0);
+    s.Phi = s.bits + (p.lists ? kBitsRing * kBitsBytes : 0);
     s.f = carve_floats(s.Phi + p.p_stages * p.b.stage_bytes, p.b, GGeo<K>::UW);
     return s;
 }
@@ -132,7 +151,115 @@ __device__ __forceinline__ bool load_barrier_and(bool ok)
 
 // ---- load warps ---------------------------------------------------------------------------------------------------------------
 
-template <bool FAST> __device__ __forceinline__ void load_role(const CUtensorMap* map, const RoleParams& p, RoleCtl& ctl, uint8_t* sPhi, int tid)
+// The bits of four pixels (0 .. 15) as two words of 16-bit masks: bit i to the sign of byte i, and the signs over the halves.
+__device__ __forceinline__ void mask_four(uint32_t b, uint32_t& m01, uint32_t& m23)
+{
+    const uint32_t signs = b * 0x10204080u;
+    asm("prmt.b32 %0, %1, 0, 0x9988;" : "=r"(m01) : "r"(signs));
+    asm("prmt.b32 %0, %1, 0, 0xBBAA;" : "=r"(m23) : "r"(signs));
+}
+
+// Lists over whole planes: a row's planes land by TMA like those of the dense form, a warp takes 64 of its pixels, sets a bit for every
+// (atom, pixel) that a list names, and clears the values without one in place; the result warps read the same bits. All planes are read for
+// a few of each pixel's, but gathering those, two bytes at a time, waits for memory twice a row (1080p x4, D = 72, k = 5, s = 8: both
+// gradients 554 us, coefficients 287, dictionary 306; so 250, 166, 158). The instructions of a row's bits and masks are too many for one
+// pair of warps (335, 199, 286): three take a row each in turn.
+__device__ __forceinline__ void load_lists(const CUtensorMap* map, const RoleParams& p, RoleCtl& ctl, uint8_t* sPhi, uint8_t* sBits, int tid)
+{
+    const Problem& pb = p.b.g.pb;
+    volatile WaitCtx* wc = &ctl.c.wait;
+    const int warp = __shfl_sync(0xffffffffu, tid >> 5, 0) & 1, lane = tid & 31, s = pb.s;
+    const int64_t HW = (int64_t)pb.H * pb.W;
+    bool ok = true;
+    int issued = -1;                                         // the last row asked for (in the pair's stage: the ones before have landed)
+    auto issue = [&](int x0, int y, int f, int item) {
+        if (warp != 0 || !p.want_dict) return;
+        const int st = item % p.p_stages;
+        ok = wait_all(&ctl.p_empty[st], ((item / p.p_stages) & 1) ^ 1, wc, ok);
+        if (!ok) return;
+        if (elect_one()) {
+            uint8_t* dst = sPhi + st * p.b.stage_bytes;
+            mbar_arrive_expect_tx(&ctl.p_land[st], (uint32_t)p.b.rows * 256u);
+            tma_load_4d(dst, map, &ctl.p_land[st], x0, y, 0, f);
+            tma_load_4d(dst + p.b.chunk_bytes, map, &ctl.p_land[st], x0 + 64, y, 0, f);
+        }
+        __syncwarp();
+        issued = item;
+    };
+    // Sixteen ranks of the row: a lane takes four pixels of every other one (idx on four bytes, W % 8 == 0: all four inside or none).
+    const int px = 4 * (lane & 15), odd = lane >> 4;
+    uint32_t a[8];
+    auto ask = [&](int x0, int y, int f, int q0) {
+        const int x = x0 + 64 * warp + px;
+        const uint8_t* at = p.b.idx + ((int64_t)f * s + q0 + odd) * HW + (int64_t)y * pb.W + x;
+#pragma unroll
+        for (int i = 0; i < 8; ++i, at += 2 * HW) a[i] = q0 + 2 * i + odd < s && x < pb.W ? __ldg(reinterpret_cast<const uint32_t*>(at)) : 0u;
+    };
+    // rows pair, pair + pairs, ... of the block's
+    const int ring = 2 * p.lists;
+    Tiles tl(p.b.g);
+    int row = tid / kLoadThreads, x0, y, f, item;
+    if (row >= p.lists) return;
+    auto settle = [&]() { while (tl.more(p.b.g) && row >= tl.rows) { row -= tl.rows; tl.next(p.b.g); } };
+    auto take = [&]() { x0 = tl.x0; y = tl.y0 + row; f = tl.f; item = tl.base + row; };
+    settle();
+    take();
+    if (tl.more(p.b.g)) {
+        issue(x0, y, f, item);
+        ask(x0, y, f, 0);
+    }
+    while (tl.more(p.b.g) && ok) {
+        const int bst = item % ring;
+        if (p.want_coef) ok = wait_all(&ctl.b_empty[bst], ((item / ring) & 1) ^ 1, wc, ok);
+        if (!ok) break;
+        uint32_t* bits = reinterpret_cast<uint32_t*>(sBits + bst * kBitsBytes) + warp * 256;     // of the warp's pixels: [32 pixels][atom]
+#pragma unroll
+        for (int i = 0; i < 2; ++i) reinterpret_cast<uint4*>(bits)[lane + 32 * i] = make_uint4(0u, 0u, 0u, 0u);
+        __syncwarp();
+        uint32_t* word = bits + (px >> 5) * 128;
+        const uint32_t first = x0 + 64 * warp + px < pb.W ? 1u << (px & 31) : 0u;
+        for (int q0 = 0;; ) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (q0 + 2 * i < s) {
+                    const uint32_t bit = q0 + 2 * i + odd < s ? first : 0u;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) atomicOr(word + min((int)(a[i] >> (8 * j) & 255u), pb.D - 1), bit << j);
+                }
+            if ((q0 += 16) >= s) break;
+            ask(x0, y, f, q0);
+        }
+        const int at_row = item;
+        row += p.lists;
+        settle();
+        take();
+        if (tl.more(p.b.g)) ask(x0, y, f, 0);
+        __syncwarp();
+        if (p.want_coef) mbar_arrive(&ctl.b_full[bst]);
+        if (!p.want_dict) continue;
+        const int st = at_row % p.p_stages;
+        if (!(ok = wait_all(&ctl.p_land[st], (at_row / p.p_stages) & 1, wc, ok))) break;
+        uint8_t* chunk = sPhi + st * p.b.stage_bytes + warp * p.b.chunk_bytes;
+        const int unit = lane & 7;
+#pragma unroll 4
+        for (int l = lane >> 3; l < pb.D; l += 4) {
+            const uint32_t b = reinterpret_cast<const uint8_t*>(bits)[(unit >> 2) * 512 + l * 4 + (unit & 3)];
+            uint4* at = reinterpret_cast<uint4*>(chunk + l * 128 + ((unit ^ (l & 7)) << 4));
+            uint4 v = *at;
+            uint32_t m0, m1, m2, m3;
+            mask_four(b & 15u, m0, m1);
+            mask_four(b >> 4, m2, m3);
+            *at = make_uint4(v.x & m0, v.y & m1, v.z & m2, v.w & m3);
+        }
+        fence_proxy_async_smem();
+        mbar_arrive(&ctl.p_full[st]);
+        if (tl.more(p.b.g)) issue(x0, y, f, item);
+    }
+    // what was asked for lands before shared memory is given up
+    if (!ok && issued >= 0) mbar_wait_drain(&ctl.p_land[issued % p.p_stages], (issued / p.p_stages) & 1);
+}
+
+template <Form FORM> __device__ __forceinline__ void load_role(const CUtensorMap* map, const RoleParams& p, RoleCtl& ctl, uint8_t* sPhi, int tid)
 {
     const Problem& pb = p.b.g.pb;
     volatile WaitCtx* wc = &ctl.c.wait;
@@ -157,7 +284,7 @@ template <bool FAST> __device__ __forceinline__ void load_role(const CUtensorMap
             mbar_wait_drain(&ctl.p_full[item % p.p_stages], (item / p.p_stages) & 1);
         return;
     }
-    if (FAST || p.copy_bytes) {
+    if (FORM == kFast || p.copy_bytes) {
         // asynchronous copies of 16, 8 or 4 bytes (eight pixels to two): planes picked one by one, widths and addresses TMA does not take
         const int px = p.copy_bytes / 2, per = 128 / px, total = per * p.b.rows;
         const bool pick = p.b.mode == kModeGlobal && !(pb.flags & SR_COEF_COMPACT);
@@ -306,7 +433,7 @@ __device__ __forceinline__ void times2(float& x, float& y, float a, float b, flo
 
 // ---- result warps ---------------------------------------------------------------------------------------------------------------
 
-template <int K, bool FAST> __device__ __forceinline__ void result_role(const CUtensorMap* map, const RoleParams& p, RoleCtl& ctl, const RoleSmem<K>& s, uint32_t tmem, int grp, int tid)
+template <int K, Form FORM> __device__ __forceinline__ void result_role(const CUtensorMap* map, const RoleParams& p, RoleCtl& ctl, const RoleSmem<K>& s, uint32_t tmem, int grp, int tid)
 {
     using G = GGeo<K>;
     const Problem& pb = p.b.g.pb;
@@ -316,7 +443,7 @@ template <int K, bool FAST> __device__ __forceinline__ void result_role(const CU
     const int64_t HW = (int64_t)pb.H * W;
     const uint32_t at = tmem + ((uint32_t)(32 * warp) << 16), acc_at = at + grp * 128;
     constexpr int STEP = K == 7 ? 16 : 32;                   // accumulator columns at a time (registers)
-    const bool listed = !FAST && p.b.mode == kModeIdx, compact = !FAST && p.b.mode == kModeCompact;
+    const bool listed = FORM == kGeneral && p.b.mode == kModeIdx, compact = FORM == kGeneral && p.b.mode == kModeCompact;
     const bool together = p.want_coef && (listed || compact);        // these meet at barriers, so they leave together
     const bool mine = 32 * warp < p.atoms;                   // this warp has atoms
     const float back = p.want_coef && l < p.atoms ? ctl.back[l] : 0.f;
@@ -343,6 +470,14 @@ template <int K, bool FAST> __device__ __forceinline__ void result_role(const CU
                         const int a = min((int)__ldg(p.b.idx + ((int64_t)tl.f * pb.s + q) * HW + pix + tid), pb.D - 1);
                         atomicOr(&ctl.listed[grp][a][tid >> 5], 1u << (tid & 31));
                     }
+            }
+            if (FORM == kLists) {
+                const int ring = 2 * p.lists, bst = item % ring;
+                ok = wait_all(&ctl.b_full[bst], (item / ring) & 1, wc, ok);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) keep[i] = reinterpret_cast<const uint32_t*>(s.bits + bst * kBitsBytes)[i * 128 + l];
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&ctl.b_empty[bst]);
             }
             ok = wait_all(&ctl.c_full[grp], (item >> 1) & 1, wc, ok);
             if (listed) {
@@ -380,12 +515,13 @@ template <int K, bool FAST> __device__ __forceinline__ void result_role(const CU
                                 const __half2 v2 = __floats2half2_rn(a, b);
                                 h[i] = *reinterpret_cast<const uint32_t*>(&v2) & whole;      // (an atom outside the subset: zeros, whatever G is)
                             }
-                            if (listed) {                    // pixels that do not list the atom
+                            if (listed || FORM == kLists) {  // pixels that do not list the atom
+                                const uint32_t b = keep[(c0 + c1 + 8 * j) / 32] >> ((c0 + c1 + 8 * j) % 32);
+                                uint32_t m[4];
+                                mask_four(b & 15u, m[0], m[1]);
+                                mask_four(b >> 4 & 15u, m[2], m[3]);
 #pragma unroll
-                                for (int i = 0; i < 4; ++i) {
-                                    const uint32_t two = keep[(c0 + c1 + 8 * j + 2 * i) / 32] >> ((c0 + c1 + 8 * j + 2 * i) % 32);
-                                    h[i] &= ((two & 1u) ? 0xFFFFu : 0u) | ((two & 2u) ? 0xFFFF0000u : 0u);
-                                }
+                                for (int i = 0; i < 4; ++i) h[i] &= m[i];
                             }
                             *reinterpret_cast<uint4*>(to + lane * 128 + (((c1 / 8 + j) ^ (lane & 7)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
                         }
@@ -407,7 +543,7 @@ template <int K, bool FAST> __device__ __forceinline__ void result_role(const CU
                             p.b.gcoef[pl] = *reinterpret_cast<const __half*>(chunk + (a >> 5) * 4096 + (a & 31) * 128 +
                                                                             ((((px >> 3) ^ (a & 7))) << 4) + (px & 7) * 2);
                         }
-                } else if (FAST || p.tma_out) {
+                } else if (FORM != kGeneral || p.tma_out) {
                     fence_proxy_async_smem();
                     __syncwarp();
                     if (lane == 0 && mine && ok && tl.x0 + c0 < W) {
@@ -484,13 +620,12 @@ template <int K, bool FAST> __device__ __forceinline__ void result_role(const CU
     }
 }
 
-// FAST: results by TMA, coefficients by TMA or asynchronous copies; without the other ways' code its roles keep their values in registers
-// (1080p x4: 188 -> 172 us).
-template <int K, bool FAST>
-__global__ void __launch_bounds__(kRoleThreads, 1)
+template <int K, Form FORM>
+__global__ void __launch_bounds__(kRoleThreads<FORM>, 1)
 grad_roles_kernel(const __grid_constant__ CUtensorMap map_in, const __grid_constant__ CUtensorMap map_out, const __grid_constant__ RoleParams p)
 {
     using G = GGeo<K>;
+    constexpr int kThreads = kRoleThreads<FORM>, kMma = kMmaWarp<FORM>;
     extern __shared__ uint8_t smem_raw[];
     __shared__ RoleCtl ctl;
     uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
@@ -498,23 +633,24 @@ grad_roles_kernel(const __grid_constant__ CUtensorMap map_in, const __grid_const
     const Problem& pb = p.b.g.pb;
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), D = pb.D;
 
-    init_ctl(ctl.c, p.b, tid, kRoleThreads, p.want_coef + p.want_dict);
+    init_ctl(ctl.c, p.b, tid, kThreads, p.want_coef + p.want_dict);
     if (tid == 0) {
         for (int i = 0; i < kMaxG; ++i) { mbar_init(&ctl.g_full[i], kGroupThreads); mbar_init(&ctl.g_empty[i], p.want_coef + p.want_dict); }
-        for (int i = 0; i < kMaxP; ++i) { mbar_init(&ctl.p_full[i], p.tma_in ? 1 : kLoadThreads); mbar_init(&ctl.p_empty[i], 1); }
+        for (int i = 0; i < kMaxP; ++i) { mbar_init(&ctl.p_full[i], p.tma_in && FORM != kLists ? 1 : kLoadThreads); mbar_init(&ctl.p_empty[i], 1); mbar_init(&ctl.p_land[i], 1); }
+        for (int i = 0; i < kBitsRing; ++i) { mbar_init(&ctl.b_full[i], kLoadThreads); mbar_init(&ctl.b_empty[i], 4); }
         for (int i = 0; i < 2; ++i) { mbar_init(&ctl.c_full[i], 1); mbar_init(&ctl.c_empty[i], 4); mbar_init(&ctl.d_full[i], 1); mbar_init(&ctl.d_empty[i], 4); }
         fence_barrier_init();
         if (p.tma_in) prefetch_tensormap(&map_in);
         if (p.tma_out) prefetch_tensormap(&map_out);
     }
     // (what the products read beyond the atoms, planes and taps written ends in lanes and columns that nobody reads)
-    for (int i = tid; i < pb.c * p.b.g.trows * p.b.g.tcols + 8; i += kRoleThreads) s.f.L[i] = 0.f;
+    for (int i = tid; i < pb.c * p.b.g.trows * p.b.g.tcols + 8; i += kThreads) s.f.L[i] = 0.f;
     if (p.b.mode == kModeGlobal && tid < pb.s) ctl.c.atoms[tid] = (uint8_t)min((int)__ldg(p.b.idx + tid), D - 1);
     __syncthreads();
     if (p.want_coef)
-        for (int q = tid; q < p.atoms; q += kRoleThreads) ctl.back[q] = write_atom<K>(p.b, s.D, p.d_block, q);
+        for (int q = tid; q < p.atoms; q += kThreads) ctl.back[q] = write_atom<K>(p.b, s.D, p.d_block, q);
     fence_proxy_async_smem();
-    if (warp == kMmaWarp) tmem_alloc(&ctl.c.tmem_base, 512);
+    if (warp == kMma) tmem_alloc(&ctl.c.tmem_base, 512);
     tc_fence_before_sync();
     __syncthreads();
     tc_fence_after_sync();
@@ -522,16 +658,17 @@ grad_roles_kernel(const __grid_constant__ CUtensorMap map_in, const __grid_const
 
     // (setmaxnreg: whole warpgroups)
     if (warp < kResultWarp) {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsG));
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsG<FORM>));
         g_role<K>(p, ctl, s, tid);
     } else if (warp < kLoadWarp) {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsResult));
-        result_role<K, FAST>(&map_out, p, ctl, s, tmem, (warp - kResultWarp) / 4, (tid - kResultWarp * 32) % kGroupThreads);
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsResult<FORM>));
+        result_role<K, FORM>(&map_out, p, ctl, s, tmem, (warp - kResultWarp) / 4, (tid - kResultWarp * 32) % kGroupThreads);
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsLoad));
-        if (warp == kMmaWarp) { if (p.want_coef) mma_role<K, true>(p, ctl, s, tmem); }
-        else if (warp == kMmaWarp + 1) { if (p.want_dict) mma_role<K, false>(p, ctl, s, tmem); }
-        else if (p.want_dict) load_role<FAST>(&map_in, p, ctl, s.Phi, tid - kLoadWarp * 32);
+        if (warp == kMma) { if (p.want_coef) mma_role<K, true>(p, ctl, s, tmem); }
+        else if (warp == kMma + 1) { if (p.want_dict) mma_role<K, false>(p, ctl, s, tmem); }
+        else if (FORM == kLists) load_lists(&map_in, p, ctl, s.Phi, s.bits, tid - kLoadWarp * 32);
+        else if (p.want_dict) load_role<FORM>(&map_in, p, ctl, s.Phi, tid - kLoadWarp * 32);
     }
 
     if (warp < kResultWarp || warp >= kLoadWarp) {
@@ -541,13 +678,15 @@ grad_roles_kernel(const __grid_constant__ CUtensorMap map_in, const __grid_const
         tc_fence_after_sync();
     }
     if (ctl.c.wait.abort_flag && tid == 0) atomicExch(p.b.status, SR_ERR_TIMEOUT);
-    if (warp == kMmaWarp) tmem_dealloc(tmem, 512);
+    if (warp == kMma) tmem_dealloc(tmem, 512);
 }
 
 // ---- host ------------------------------------------------------------------------------------------------------------------------
 
 int out_planes(const GradArgs& a) { return a.mode == kModeCompact || (a.mode == kModeGlobal && (a.pb.flags & SR_COEF_COMPACT)) ? a.pb.s : a.pb.D; }
 int product_atoms(const GradArgs& a) { return a.mode == kModeGlobal && (a.pb.flags & SR_COEF_COMPACT) ? a.pb.s : a.pb.D; }
+
+bool tma_takes(const Problem& pb, const void* at) { return pb.W % 8 == 0 && ((uintptr_t)at & 15) == 0; }
 
 // As many coefficient stages up to four as fit; at least two.
 template <int K> bool plan(RoleParams& p, const GradArgs& a, size_t& smem)
@@ -561,11 +700,12 @@ template <int K> bool plan(RoleParams& p, const GradArgs& a, size_t& smem)
     p.b.chunk_bytes = p.b.stage_bytes / 2;
     const size_t floats = float_bytes<K>(p.b.g, a.pb, a.lr);
     // (behind the atoms lie 16 KB and more of results, so what the first product reads there is shared memory)
-    const size_t fixed = 1024 + (size_t)kRing<K> * GGeo<K>::G_BYTES + (p.want_coef ? GGeo<K>::BLOCKS * p.d_block + kRG * kOutBytes : 0) + floats;
+    const size_t fixed = 1024 + (size_t)kRing<K> * GGeo<K>::G_BYTES + (p.want_coef ? GGeo<K>::BLOCKS * p.d_block + kRG * kOutBytes : 0) +
+                         (p.lists ? kBitsRing * kBitsBytes : 0) + floats;
     p.p_stages = 0;
     smem = fixed;
     if (p.want_dict) {
-        for (p.p_stages = kMaxP; p.p_stages >= 2; --p.p_stages) {
+        for (p.p_stages = p.lists ? kListPairs : kMaxP; p.p_stages >= 2; --p.p_stages) {
             smem = fixed + (size_t)p.p_stages * p.b.stage_bytes;
             // the second product reads 128 rows of a chunk, whatever lies behind the last one must be shared memory
             const size_t reach = smem - floats - p.b.chunk_bytes + 128 * 128;
@@ -573,15 +713,26 @@ template <int K> bool plan(RoleParams& p, const GradArgs& a, size_t& smem)
             if (fits(smem, kRoleReserve)) break;
         }
         if (p.p_stages < 2) return false;
+        if (p.lists) p.lists = p.p_stages;
     }
     return fits(smem, kRoleReserve);
 }
 
-template <int K, bool FAST> cudaError_t launch_form(const CUtensorMap& in, const CUtensorMap& out, const RoleParams& p, int blocks, size_t smem, cudaStream_t st)
+// With lists masked in place where that fits and TMA takes the planes.
+template <int K> bool plan_best(RoleParams& p, const GradArgs& a, size_t& smem)
+{
+    const bool ways = (!(a.gdict || a.ggamma) || tma_takes(a.pb, a.coef)) && (!a.gcoef || tma_takes(a.pb, a.gcoef));
+    p.lists = a.mode == kModeIdx && ((uintptr_t)a.idx & 3) == 0 && ways ? kListPairs : 0;
+    if (p.lists && plan<K>(p, a, smem)) return true;         // (two pairs at least: with two stages)
+    p.lists = 0;
+    return plan<K>(p, a, smem);
+}
+
+template <int K, Form FORM> cudaError_t launch_form(const CUtensorMap& in, const CUtensorMap& out, const RoleParams& p, int blocks, size_t smem, cudaStream_t st)
 {
     static bool done[64] = {false};
-    if (cudaError_t e = allow_smem(grad_roles_kernel<K, FAST>, done, kRoleReserve)) return e;
-    grad_roles_kernel<K, FAST><<<blocks, kRoleThreads, smem, st>>>(in, out, p);
+    if (cudaError_t e = allow_smem(grad_roles_kernel<K, FORM>, done, kRoleReserve)) return e;
+    grad_roles_kernel<K, FORM><<<blocks, kRoleThreads<FORM>, smem, st>>>(in, out, p);
     count_launches(1);
     return cudaGetLastError();
 }
@@ -592,28 +743,32 @@ template <int K> cudaError_t launch_k(const GradArgs& a, int* slots)
     p.b = common_params(a);
     if (!p.b.status) return cudaErrorUnknown;
     size_t smem = 0;
-    if (!plan<K>(p, a, smem)) return cudaErrorNotSupported;
+    if (!plan_best<K>(p, a, smem)) return cudaErrorNotSupported;
     p.planes_out = out_planes(a);
     p.planes_in = p.planes_out;
     CUtensorMap in{}, out{};
     const Problem& pb = a.pb;
     const bool whole = a.mode == kModeDense || (a.mode == kModeGlobal && (pb.flags & SR_COEF_COMPACT));
-    if (p.want_dict && whole && pb.W % 8 == 0 && ((uintptr_t)a.coef & 15) == 0) p.tma_in = encode_planes(&in, a.coef, pb, p.planes_in, p.b.rows);
+    if (p.want_dict && (whole || p.lists) && tma_takes(pb, a.coef)) p.tma_in = encode_planes(&in, a.coef, pb, p.planes_in, p.b.rows);
     if (p.want_dict && !p.tma_in && (whole || a.mode == kModeGlobal))
         for (int bytes = 16; bytes >= 4 && !p.copy_bytes; bytes /= 2)
             if (pb.W % (bytes / 2) == 0 && ((uintptr_t)a.coef & (bytes - 1)) == 0) p.copy_bytes = bytes;
-    if (p.want_coef && a.mode != kModeCompact && pb.W % 8 == 0 && ((uintptr_t)a.gcoef & 15) == 0) p.tma_out = encode_planes(&out, a.gcoef, pb, p.planes_out, 32);
+    if (p.want_coef && a.mode != kModeCompact && tma_takes(pb, a.gcoef)) p.tma_out = encode_planes(&out, a.gcoef, pb, p.planes_out, 32);
     p.out_pairs = pb.W % 2 == 0 && ((uintptr_t)a.gcoef & 3) == 0;
-    const bool fast = (!p.want_coef || p.tma_out) && (!p.want_dict || p.tma_in || p.copy_bytes) && a.mode != kModeIdx;
+    const bool ways = (!p.want_coef || p.tma_out) && (!p.want_dict || p.tma_in || p.copy_bytes);
+    if (p.lists && !ways) return cudaErrorUnknown;           // (no encoder of tensor maps)
     *slots = p.b.g.num_tiles < sm_count() ? p.b.g.num_tiles : sm_count();
-    return fast ? launch_form<K, true>(in, out, p, *slots, smem, a.st) : launch_form<K, false>(in, out, p, *slots, smem, a.st);
+    if (p.lists) return launch_form<K, kLists>(in, out, p, *slots, smem, a.st);
+    return ways && a.mode != kModeIdx ? launch_form<K, kFast>(in, out, p, *slots, smem, a.st) : launch_form<K, kGeneral>(in, out, p, *slots, smem, a.st);
 }
 
 template <int K> bool plan_fits(const GradArgs& a)
 {
     RoleParams p{};
     size_t smem;
-    return plan<K>(p, a, smem);
+    if (!plan_best<K>(p, a, smem)) return false;
+    // (gathered lists: see grad_roles_supported)
+    return a.gcoef || p.lists || (a.mode != kModeIdx && a.mode != kModeCompact);
 }
 
 } // namespace
@@ -622,11 +777,10 @@ bool grad_roles_supported(const GradArgs& a)
 {
     if (!form_supported(a) || a.pb.D > 128) return false;
     // Two load warps without asynchronous copies do not keep up with whole planes (odd widths: 1077 x 1080, D = 72: both gradients 686 us,
-    // 537 by the two kernels of sr_grad_tc.cu), nor with the dictionary's sums over lists alone (1080p x4, s = 8: 473 / 303; both
-    // gradients 545 / 768).
+    // 537 by the two kernels of sr_grad_tc.cu), nor with the dictionary's sums over gathered lists alone (1080p x4, s = 8: 473 / 303; both
+    // gradients 545 / 768; lists masked in place do: plan_fits).
     const bool sums = a.gdict || a.ggamma;
     if (sums && (a.mode == kModeDense || a.mode == kModeGlobal) && (a.pb.W % 2 != 0 || ((uintptr_t)a.coef & 3) != 0)) return false;
-    if (sums && !a.gcoef && (a.mode == kModeIdx || a.mode == kModeCompact)) return false;
     switch (a.pb.k) {
     case 3: return plan_fits<3>(a);
     case 5: return plan_fits<5>(a);

@@ -353,6 +353,29 @@ def test_frames_of_many_tiles_a_block(w, k, D, c, mode):
         assert float((got.double() - want).norm()) <= 2e-6 * float(magnitude.norm())
 
 
+@pytest.mark.parametrize("k,D,s", [(3, 72, 8), (5, 72, 8), (5, 72, 21), (5, 128, 8), (5, 17, 3), (7, 72, 8), (7, 32, 16)])
+def test_lists_masked_in_place_and_lists_gathered_are_the_same(k, D, s):
+    """Lists on four bytes and lists on an odd address take different ways through the kernel. Full frames, every gradient alone and both,
+    lists with atoms twice and indices behind the last atom."""
+    n, c, h, w, r = 1, 3, 270, 482, 4
+    gen = torch.Generator(device="cuda").manual_seed(100 * k + D + s)
+    lr = torch.rand((n, c, h, w), device="cuda", generator=gen)
+    coef = torch.empty((n, D, h * r, w * r), device="cuda", dtype=torch.float16).normal_(1 / D, 0.05, generator=gen)
+    g = torch.empty((n, c, h * r, w * r), device="cuda").normal_(0, 0.05, generator=gen)
+    d = torch.empty((D, k * k), device="cuda").normal_(0, 0.2, generator=gen)
+    idx = torch.randint(0, D + 4, (n, s, h * r, w * r), device="cuda", dtype=torch.uint8, generator=gen)
+    odd = torch.empty(idx.numel() + 1, device="cuda", dtype=torch.uint8)[1:].view(idx.shape)
+    odd.copy_(idx)
+    call = lambda i, **kw: sr.sr_dict_regress_selected_grad(lr, coef, i, None, d, g, r, k, s, **kw)[:2]  # noqa: E731
+    gc, gd = call(odd)
+    for _ in range(3):
+        for got, want in zip(call(idx) + call(idx, want_dict=False)[:1] + call(idx, want_coef=False)[1:], (gc, gd, gc, gd)):
+            assert torch.equal(got, want) if got.dim() == 4 else float((got - want).norm()) <= 2e-6 * float(want.norm())
+    assert sr.sr_device_status() == 0
+    listed = torch.zeros((D, h * r, w * r), device="cuda", dtype=torch.bool).scatter_(0, idx[0].long().clamp_(max=D - 1), True)
+    assert bool((gc[0][~listed] == 0).all()) and bool((gc[0][listed] != 0).float().mean() > 0.99)
+
+
 @pytest.mark.parametrize("case", ["dense", "listed", "more atoms", "odd width"])
 def test_a_wait_that_runs_out_is_reported_and_the_next_call_is_clean(case):
     """One product's completion is never announced (the hook of the forward calls): the block gives up, nothing hangs, the status says so."""
