@@ -19,7 +19,7 @@ constexpr int TX = 32, CCHUNK = 4;
 template <int K> struct KK { static constexpr int value = K * K, padded = (K * K + 3) & ~3; };
 
 // Up-sampled tile of TX x TY pixels with its halo, CCHUNK channels at a time, in shared memory: the vertical taps on the LR columns that
-// the tile reads, then the horizontal ones. (Sixteen taps a value, straight from memory, were a third of these kernels' instructions.)
+// the tile reads, then the horizontal ones.
 template <int K, int TY> struct UTile {
     static constexpr int P = (K - 1) / 2, UW = TX + 2 * P, UH = TY + 2 * P, LC = UW + 4;      // LR columns: most at scale 1
     float u[CCHUNK * UH * UW];
@@ -100,7 +100,7 @@ grad_coef_kernel(const __grid_constant__ CoefGradParams p, CoefT* __restrict__ g
     const int64_t HW = (int64_t)H * W;
     const bool compact = p.mode == kModeCompact || (p.mode == kModeGlobal && (pb.flags & SR_COEF_COMPACT));
 
-    let_next_launch_start();                     // the dictionary's sums, which need nothing of this (128 x 128, fp32: 37 -> 24 us)
+    let_next_launch_start();                     // the dictionary's sums, which need nothing of this (128 x 128, fp32: 37 -> 29 us)
     for (int i = tid; i < D * kkp; i += 256) {
         const int l = i / kkp, j = i - l * kkp;
         sdict[i] = j < kk ? __ldg(p.dict + (int64_t)l * kk + j) : 0.f;
@@ -234,7 +234,7 @@ grad_dict_kernel(const __grid_constant__ DictGradParams p, const CoefT* __restri
 
     for (int i = tid; i < kkp * PITCH; i += 256) sG[i] = 0.f;
     for (int i = tid; i < phi * (p.ahead ? 2 : 1); i += 256) sPhi[i] = 0.f;
-    // A tile's planes by asynchronous copies of `ahead` bytes, a tile ahead (fp32, whole planes): 1080p x4, D = 72: 1584 -> 620 us.
+    // A tile's planes by asynchronous copies of `ahead` bytes, a tile ahead (fp32, whole planes): 1080p x4, D = 72: 1584 -> 743 us.
     auto fetch = [&](int t, float* to) {
         const int per = p.tiles_x * p.tiles_y;
         const int f = t / per, rest = t - f * per;

@@ -5,12 +5,12 @@
 // (1080p x4, D = 72, k = 5: 129 + 129 us in two kernels, 34 of each the up-sampled tile, against 95 us of traffic). Here one block per
 // multiprocessor holds a pipeline, and G, which costs most, is computed once for both products:
 //   G warps (kFG groups of four)   the up-sampled tile; G of every row, hi + lo, into a ring of tiles         g_full
-//   load warps (two; lists: six)   the row's coefficients into a ring of stages: TMA boxes (lists: masked      p_full
+//   load warps (two or six)         the row's coefficients into a ring of stages: TMA boxes (lists: masked      p_full
 //                                  there), or (widths and addresses TMA does not take, gathered planes,
 //                                  compact values) smaller asynchronous copies or a pixel a thread
 //   MMA warps (one a product)      a row's coefficient gradients in one of two accumulators (lane = atom,     c_full, g_empty
-//                                  column = pixel), the dictionary's sums over the tile in one of two more     d_full, p_empty, g_empty
-//   result warps (kRG groups of four)  a row's coefficient gradients to memory (c_empty), the tile's dictionary sums to registers (d_empty)
+//                                  column = pixel), the dictionary's sums over four rows in one of two more    d_full, p_empty, g_empty
+//   result warps (kRG groups of four)  a row's coefficient gradients to memory (c_empty), those dictionary sums to registers (d_empty)
 // Rows are numbered through the block's tiles; row i goes to G group i mod kFG, ring entries i mod their count, accumulator i mod 2.
 // Waits suspend (mbar_wait): warps with time to spare must not take issue slots from those that set the pace.
 // Every wait is bounded: on expiry a warp raises the block's flag and leaves its loop, as every other does at its next wait.
@@ -27,23 +27,25 @@ using namespace gradtc;
 constexpr int kFG = 2;                                       // groups of G warps
 constexpr int kRG = 2;                                       // groups of result warps: rows of one accumulator each
 // What a kernel is compiled for. kFast: results by TMA, coefficients by TMA or asynchronous copies; without the other ways' code its roles
-// keep their values in registers (1080p x4: 188 -> 162 us). kLists: lists, both by TMA. kGeneral: the rest.
-enum Form { kGeneral, kFast, kLists };
+// keep their values in registers (1080p x4: 188 -> 162 us). kLists: lists, both by TMA. kGeneral: the rest. kPairs: the same with
+// more load warps and fewer registers a warp.
+enum Form { kGeneral, kPairs, kFast, kLists };
+constexpr bool has_pairs(Form f) { return f == kPairs || f == kLists; }
 constexpr int kResultWarp = kFG * 4, kLoadWarp = kResultWarp + kRG * 4, kLoadThreads = 64;
-constexpr int kListPairs = 3;                                // pairs of load warps of kLists: a row a pair, in turn
-template <Form F> constexpr int kMmaWarp = kLoadWarp + (F == kLists ? 2 * kListPairs : 2);
+constexpr int kLoadPairs = 3;                                // pairs of load warps where there are more than one: a row a pair, in turn
+template <Form F> constexpr int kMmaWarp = kLoadWarp + (has_pairs(F) ? 2 * kLoadPairs : 2);
 template <Form F> constexpr int kRoleThreads = (kMmaWarp<F> + 2) * 32;
 // Registers a thread: of the launch, and after the G warps have taken what the others do not need (whole warpgroups; an increase beyond
 // what the block was launched with would wait for ever).
-template <Form F> constexpr int kRegsLaunch = F == kLists ? 80 : 96;
-template <Form F> constexpr int kRegsG = F == kLists ? 104 : 112;
-template <Form F> constexpr int kRegsResult = F == kLists ? 88 : 104;
+template <Form F> constexpr int kRegsLaunch = has_pairs(F) ? 80 : 96;
+template <Form F> constexpr int kRegsG = has_pairs(F) ? 104 : 112;
+template <Form F> constexpr int kRegsResult = has_pairs(F) ? 88 : 104;
 constexpr int kRegsLoad = 48;
 template <Form F> constexpr bool kRegsFit =
     kRegsG<F> >= kRegsLaunch<F> && kRegsResult<F> >= kRegsLaunch<F> && kRegsLoad <= kRegsLaunch<F> &&   // inc, inc, dec: the other direction is illegal
     kRoleThreads<F> % 128 == 0 && kRegsLaunch<F> * kRoleThreads<F> <= 65536 &&
     128 * (kFG * kRegsG<F> + kRG * kRegsResult<F> + (kRoleThreads<F> / 128 - kFG - kRG) * kRegsLoad) <= kRegsLaunch<F> * kRoleThreads<F>;
-static_assert(kRegsFit<kGeneral> && kRegsFit<kFast> && kRegsFit<kLists>, "the roles' registers are the launch's");
+static_assert(kRegsFit<kGeneral> && kRegsFit<kPairs> && kRegsFit<kFast> && kRegsFit<kLists>, "the roles' registers are the launch's");
 constexpr int kRoleReserve = 6656;                           // static shared memory, kept out of the dynamic budget
 constexpr int kMaxG = 4, kMaxP = 4, kUnscales = 16;
 // Rows whose dictionary sums stay in tensor memory: its additions cut off, so every one shrinks the sum by a third of 2^-24 (8 rows, 64
@@ -55,7 +57,7 @@ __device__ __forceinline__ int segments(int rows) { return (rows + kSegment - 1)
 template <int K> constexpr int kRing = K == 7 ? 2 : kMaxG;
 // Lists: rows of bits, one for each of a row's pixels and 128 atoms. Every stage has one pair of load warps, and every entry of bits one pair
 // and one result group (two entries a pair), for the same reason: a wait for the use before follows that warp's own use before.
-constexpr int kBitsRing = 2 * kListPairs, kBitsBytes = 128 * 16;
+constexpr int kBitsRing = 2 * kLoadPairs, kBitsBytes = 128 * 16;
 static_assert(kRG == 2, "two entries a pair");
 static_assert(kRing<7> >= kFG && kRing<5> >= kFG, "a group is never two uses ahead of a ring entry");
 
@@ -79,8 +81,8 @@ struct RoleParams {
     int out_pairs;               // results stored two pixels at a time (where not by TMA)
     int copy_bytes;              // coefficients by asynchronous copies of this size; 0 = TMA or one by one
     int want_coef, want_dict;
-    int lists;                   // lists over planes that TMA takes: pairs of load warps that mask them, and make the bits for the result warps;
-                                 // as many as stages
+    int lists;                   // lists over planes that TMA takes: the load warps mask them, and make the bits for the result warps
+    int pairs;                   // of load warps at work; if more than one, as many as stages
 };
 
 template <int K> struct RoleSmem {
@@ -141,11 +143,11 @@ template <int K> __device__ __forceinline__ bool g_role(const RoleParams& p, Rol
     return ok;
 }
 
-__device__ __forceinline__ bool load_barrier_and(bool ok)
+__device__ __forceinline__ bool load_barrier_and(int pair, bool ok)
 {
     int r;
-    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\tbarrier.cta.red.and.pred q, 6, %2, p;\n\tselp.b32 %0, 1, 0, q;\n\t}"
-                 : "=r"(r) : "r"((int)ok), "n"(kLoadThreads) : "memory");
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\tbarrier.cta.red.and.pred q, %3, %2, p;\n\tselp.b32 %0, 1, 0, q;\n\t}"
+                 : "=r"(r) : "r"((int)ok), "n"(kLoadThreads), "r"(6 + pair) : "memory");
     return r != 0;
 }
 
@@ -196,10 +198,10 @@ __device__ __forceinline__ void load_lists(const CUtensorMap* map, const RolePar
         for (int i = 0; i < 8; ++i, at += 2 * HW) a[i] = q0 + 2 * i + odd < s && x < pb.W ? __ldg(reinterpret_cast<const uint32_t*>(at)) : 0u;
     };
     // rows pair, pair + pairs, ... of the block's
-    const int ring = 2 * p.lists;
+    const int ring = 2 * p.pairs;
     Tiles tl(p.b.g);
     int row = tid / kLoadThreads, x0, y, f, item;
-    if (row >= p.lists) return;
+    if (row >= p.pairs) return;
     auto settle = [&]() { while (tl.more(p.b.g) && row >= tl.rows) { row -= tl.rows; tl.next(p.b.g); } };
     auto take = [&]() { x0 = tl.x0; y = tl.y0 + row; f = tl.f; item = tl.base + row; };
     settle();
@@ -230,7 +232,7 @@ __device__ __forceinline__ void load_lists(const CUtensorMap* map, const RolePar
             ask(x0, y, f, q0);
         }
         const int at_row = item;
-        row += p.lists;
+        row += p.pairs;
         settle();
         take();
         if (tl.more(p.b.g)) ask(x0, y, f, 0);
@@ -264,7 +266,10 @@ template <Form FORM> __device__ __forceinline__ void load_role(const CUtensorMap
     const Problem& pb = p.b.g.pb;
     volatile WaitCtx* wc = &ctl.c.wait;
     const int64_t HW = (int64_t)pb.H * pb.W;
-    if (p.tma_in) {
+    const int pair = FORM == kPairs ? __shfl_sync(0xffffffffu, tid >> 6, 0) : 0;
+    if (pair >= p.pairs) return;
+    tid &= kLoadThreads - 1;
+    if (FORM != kPairs && p.tma_in) {
         // one lane: two boxes a row, bytes counted on the stage's barrier
         if ((tid >> 5) != 0 || !elect_one()) return;
         bool ok = true;
@@ -284,7 +289,7 @@ template <Form FORM> __device__ __forceinline__ void load_role(const CUtensorMap
             mbar_wait_drain(&ctl.p_full[item % p.p_stages], (item / p.p_stages) & 1);
         return;
     }
-    if (FORM == kFast || p.copy_bytes) {
+    if (FORM == kFast || (FORM != kPairs && p.copy_bytes)) {
         // asynchronous copies of 16, 8 or 4 bytes (eight pixels to two): planes picked one by one, widths and addresses TMA does not take
         const int px = p.copy_bytes / 2, per = 128 / px, total = per * p.b.rows;
         const bool pick = p.b.mode == kModeGlobal && !(pb.flags & SR_COEF_COMPACT);
@@ -314,52 +319,53 @@ template <Form FORM> __device__ __forceinline__ void load_role(const CUtensorMap
     const bool gather = p.b.mode == kModeGlobal && !(pb.flags & SR_COEF_COMPACT);      // (odd widths)
     const __half zero = __ushort_as_half(0);
     bool ok = true;
-    for (Tiles tl(p.b.g); tl.more(p.b.g); tl.next(p.b.g)) {
-        for (int row = 0; row < tl.rows; ++row) {
-            const int item = tl.base + row, st = item % p.p_stages;
-            uint8_t* stage = sPhi + st * p.b.stage_bytes;
-            ok = wait_all(&ctl.p_empty[st], ((item / p.p_stages) & 1) ^ 1, wc, ok);
+    Tiles tl(p.b.g);
+    for (int row = pair; tl.more(p.b.g); row += p.pairs) {
+        while (tl.more(p.b.g) && row >= tl.rows) { row -= tl.rows; tl.next(p.b.g); }
+        if (!tl.more(p.b.g)) break;
+        const int item = tl.base + row, st = item % p.p_stages;
+        uint8_t* stage = sPhi + st * p.b.stage_bytes;
+        ok = wait_all(&ctl.p_empty[st], ((item / p.p_stages) & 1) ^ 1, wc, ok);
+        if (lists) {
+            if (ok)
+                for (int i = tid; i < p.b.stage_bytes / 16; i += kLoadThreads) reinterpret_cast<uint4*>(stage)[i] = make_uint4(0, 0, 0, 0);
+            ok = load_barrier_and(pair, ok);                         // (a pair leaves together: its warps meet here)
+        }
+        if (!ok) return;
+        for (int x = tid; x < 128; x += kLoadThreads) {
+            const bool inside = tl.x0 + x < pb.W;
+            uint8_t* chunk = stage + (x >> 6) * p.b.chunk_bytes;
+            const int unit = (x & 63) >> 3, at2 = (x & 7) * 2;       // this pixel's 16-byte unit and place in it
+            auto place = [&](int l) { return reinterpret_cast<__half*>(chunk + l * 128 + ((unit ^ (l & 7)) << 4) + at2); };
+            const int64_t pix = (int64_t)(tl.y0 + row) * pb.W + tl.x0 + x;
+            const __half* src = p.b.coef + (int64_t)tl.f * p.planes_in * HW + pix;
             if (lists) {
-                if (ok)
-                    for (int i = tid; i < p.b.stage_bytes / 16; i += kLoadThreads) reinterpret_cast<uint4*>(stage)[i] = make_uint4(0, 0, 0, 0);
-                ok = load_barrier_and(ok);                               // (the load warps leave together: they meet here)
-            }
-            if (!ok) return;
-            for (int x = tid; x < 128; x += kLoadThreads) {
-                const bool inside = tl.x0 + x < pb.W;
-                uint8_t* chunk = stage + (x >> 6) * p.b.chunk_bytes;
-                const int unit = (x & 63) >> 3, at2 = (x & 7) * 2;       // this pixel's 16-byte unit and place in it
-                auto place = [&](int l) { return reinterpret_cast<__half*>(chunk + l * 128 + ((unit ^ (l & 7)) << 4) + at2); };
-                const int64_t pix = (int64_t)(tl.y0 + row) * pb.W + tl.x0 + x;
-                const __half* src = p.b.coef + (int64_t)tl.f * p.planes_in * HW + pix;
-                if (lists) {
-                    const uint8_t* list = p.b.idx + (int64_t)tl.f * s * HW + pix;
-                    for (int q0 = 0; inside && q0 < s; q0 += 8) {
-                        int a[8];
-                        __half v[8];
+                const uint8_t* list = p.b.idx + (int64_t)tl.f * s * HW + pix;
+                for (int q0 = 0; inside && q0 < s; q0 += 8) {
+                    int a[8];
+                    __half v[8];
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) a[i] = q0 + i < s ? min((int)__ldg(list + (int64_t)(q0 + i) * HW), pb.D - 1) : 0;
+                    for (int i = 0; i < 8; ++i) a[i] = q0 + i < s ? min((int)__ldg(list + (int64_t)(q0 + i) * HW), pb.D - 1) : 0;
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) v[i] = q0 + i < s ? __ldg(src + (int64_t)(p.b.mode == kModeCompact ? q0 + i : a[i]) * HW) : zero;
+                    for (int i = 0; i < 8; ++i) v[i] = q0 + i < s ? __ldg(src + (int64_t)(p.b.mode == kModeCompact ? q0 + i : a[i]) * HW) : zero;
 #pragma unroll
-                        for (int i = 0; i < 8; ++i)
-                            if (q0 + i < s) *place(a[i]) = v[i];
-                    }
-                } else {
-                    for (int l0 = 0; l0 < p.b.rows; l0 += 16) {
-                        __half h[16];
+                    for (int i = 0; i < 8; ++i)
+                        if (q0 + i < s) *place(a[i]) = v[i];
+                }
+            } else {
+                for (int l0 = 0; l0 < p.b.rows; l0 += 16) {
+                    __half h[16];
 #pragma unroll
-                        for (int i = 0; i < 16; ++i)
-                            h[i] = inside && l0 + i < p.b.rows ? __ldg(src + (int64_t)(gather ? ctl.c.atoms[l0 + i] : l0 + i) * HW) : zero;
+                    for (int i = 0; i < 16; ++i)
+                        h[i] = inside && l0 + i < p.b.rows ? __ldg(src + (int64_t)(gather ? ctl.c.atoms[l0 + i] : l0 + i) * HW) : zero;
 #pragma unroll
-                        for (int i = 0; i < 16; ++i)
-                            if (l0 + i < p.b.rows) *place(l0 + i) = h[i];
-                    }
+                    for (int i = 0; i < 16; ++i)
+                        if (l0 + i < p.b.rows) *place(l0 + i) = h[i];
                 }
             }
-            fence_proxy_async_smem();
-            mbar_arrive(&ctl.p_full[st]);
         }
+        fence_proxy_async_smem();
+        mbar_arrive(&ctl.p_full[st]);
     }
 }
 
@@ -443,7 +449,8 @@ template <int K, Form FORM> __device__ __forceinline__ void result_role(const CU
     const int64_t HW = (int64_t)pb.H * W;
     const uint32_t at = tmem + ((uint32_t)(32 * warp) << 16), acc_at = at + grp * 128;
     constexpr int STEP = K == 7 ? 16 : 32;                   // accumulator columns at a time (registers)
-    const bool listed = FORM == kGeneral && p.b.mode == kModeIdx, compact = FORM == kGeneral && p.b.mode == kModeCompact;
+    constexpr bool any = FORM == kGeneral || FORM == kPairs;
+    const bool listed = any && p.b.mode == kModeIdx, compact = any && p.b.mode == kModeCompact;
     const bool together = p.want_coef && (listed || compact);        // these meet at barriers, so they leave together
     const bool mine = 32 * warp < p.atoms;                   // this warp has atoms
     const float back = p.want_coef && l < p.atoms ? ctl.back[l] : 0.f;
@@ -472,7 +479,7 @@ template <int K, Form FORM> __device__ __forceinline__ void result_role(const CU
                     }
             }
             if (FORM == kLists) {
-                const int ring = 2 * p.lists, bst = item % ring;
+                const int ring = 2 * p.pairs, bst = item % ring;
                 ok = wait_all(&ctl.b_full[bst], (item / ring) & 1, wc, ok);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) keep[i] = reinterpret_cast<const uint32_t*>(s.bits + bst * kBitsBytes)[i * 128 + l];
@@ -543,7 +550,7 @@ template <int K, Form FORM> __device__ __forceinline__ void result_role(const CU
                             p.b.gcoef[pl] = *reinterpret_cast<const __half*>(chunk + (a >> 5) * 4096 + (a & 31) * 128 +
                                                                             ((((px >> 3) ^ (a & 7))) << 4) + (px & 7) * 2);
                         }
-                } else if (FORM != kGeneral || p.tma_out) {
+                } else if (!any || p.tma_out) {
                     fence_proxy_async_smem();
                     __syncwarp();
                     if (lane == 0 && mine && ok && tl.x0 + c0 < W) {
@@ -705,7 +712,7 @@ template <int K> bool plan(RoleParams& p, const GradArgs& a, size_t& smem)
     p.p_stages = 0;
     smem = fixed;
     if (p.want_dict) {
-        for (p.p_stages = p.lists ? kListPairs : kMaxP; p.p_stages >= 2; --p.p_stages) {
+        for (p.p_stages = p.pairs > 1 ? kLoadPairs : kMaxP; p.p_stages >= 2; --p.p_stages) {
             smem = fixed + (size_t)p.p_stages * p.b.stage_bytes;
             // the second product reads 128 rows of a chunk, whatever lies behind the last one must be shared memory
             const size_t reach = smem - floats - p.b.chunk_bytes + 128 * 128;
@@ -713,18 +720,35 @@ template <int K> bool plan(RoleParams& p, const GradArgs& a, size_t& smem)
             if (fits(smem, kRoleReserve)) break;
         }
         if (p.p_stages < 2) return false;
-        if (p.lists) p.lists = p.p_stages;
+        if (p.pairs > 1) p.pairs = p.p_stages;
     }
     return fits(smem, kRoleReserve);
 }
 
+// Bytes of an asynchronous copy that W and the address of the planes take, or 0.
+int copy_of(const Problem& pb, const void* at)
+{
+    for (int bytes = 16; bytes >= 4; bytes /= 2)
+        if (pb.W % (bytes / 2) == 0 && ((uintptr_t)at & (bytes - 1)) == 0) return bytes;
+    return 0;
+}
+
+// Whole planes that lanes load pixel by pixel (odd widths): from how many on three pairs of load warps beat the two kernels of
+// sr_grad_tc.cu, whose every warp loads. Both gradients, 1077 x 1080, k = 5, two kernels / pairs: D = 32: 224 / 249 us, 40: 269 / 269,
+// 56: 325 / 286, 72: 538 / 310. (One pair: D = 72: 686.) Compact values and lists, 1080p x4, D = 72, s = 8, one pair / three: compact
+// 423 / 310, its dictionary sums alone 202 (two kernels' form) / 181; at k = 7 507 / 355, 699 / 265.
+constexpr int kPairsPlanes = 40;
+bool one_by_one(const GradArgs& a) { return (a.gdict || a.ggamma) && a.mode != kModeIdx && a.mode != kModeCompact && copy_of(a.pb, a.coef) == 0; }
+
 // With lists masked in place where that fits and TMA takes the planes.
 template <int K> bool plan_best(RoleParams& p, const GradArgs& a, size_t& smem)
 {
-    const bool ways = (!(a.gdict || a.ggamma) || tma_takes(a.pb, a.coef)) && (!a.gcoef || tma_takes(a.pb, a.gcoef));
-    p.lists = a.mode == kModeIdx && ((uintptr_t)a.idx & 3) == 0 && ways ? kListPairs : 0;
-    if (p.lists && plan<K>(p, a, smem)) return true;         // (two pairs at least: with two stages)
+    const bool sums = a.gdict || a.ggamma;
+    p.pairs = kLoadPairs;
+    p.lists = a.mode == kModeIdx && ((uintptr_t)a.idx & 3) == 0 && (!sums || tma_takes(a.pb, a.coef)) && (!a.gcoef || tma_takes(a.pb, a.gcoef));
+    if (p.lists && plan<K>(p, a, smem)) return true;
     p.lists = 0;
+    p.pairs = sums && (a.mode == kModeIdx || a.mode == kModeCompact || one_by_one(a)) ? kLoadPairs : 1;
     return plan<K>(p, a, smem);
 }
 
@@ -751,14 +775,14 @@ template <int K> cudaError_t launch_k(const GradArgs& a, int* slots)
     const bool whole = a.mode == kModeDense || (a.mode == kModeGlobal && (pb.flags & SR_COEF_COMPACT));
     if (p.want_dict && (whole || p.lists) && tma_takes(pb, a.coef)) p.tma_in = encode_planes(&in, a.coef, pb, p.planes_in, p.b.rows);
     if (p.want_dict && !p.tma_in && (whole || a.mode == kModeGlobal))
-        for (int bytes = 16; bytes >= 4 && !p.copy_bytes; bytes /= 2)
-            if (pb.W % (bytes / 2) == 0 && ((uintptr_t)a.coef & (bytes - 1)) == 0) p.copy_bytes = bytes;
+        p.copy_bytes = copy_of(pb, a.coef);
     if (p.want_coef && a.mode != kModeCompact && tma_takes(pb, a.gcoef)) p.tma_out = encode_planes(&out, a.gcoef, pb, p.planes_out, 32);
     p.out_pairs = pb.W % 2 == 0 && ((uintptr_t)a.gcoef & 3) == 0;
     const bool ways = (!p.want_coef || p.tma_out) && (!p.want_dict || p.tma_in || p.copy_bytes);
     if (p.lists && !ways) return cudaErrorUnknown;           // (no encoder of tensor maps)
     *slots = p.b.g.num_tiles < sm_count() ? p.b.g.num_tiles : sm_count();
     if (p.lists) return launch_form<K, kLists>(in, out, p, *slots, smem, a.st);
+    if (p.pairs > 1) return launch_form<K, kPairs>(in, out, p, *slots, smem, a.st);
     return ways && a.mode != kModeIdx ? launch_form<K, kFast>(in, out, p, *slots, smem, a.st) : launch_form<K, kGeneral>(in, out, p, *slots, smem, a.st);
 }
 
@@ -766,9 +790,7 @@ template <int K> bool plan_fits(const GradArgs& a)
 {
     RoleParams p{};
     size_t smem;
-    if (!plan_best<K>(p, a, smem)) return false;
-    // (gathered lists: see grad_roles_supported)
-    return a.gcoef || p.lists || (a.mode != kModeIdx && a.mode != kModeCompact);
+    return plan_best<K>(p, a, smem);
 }
 
 } // namespace
@@ -776,11 +798,7 @@ template <int K> bool plan_fits(const GradArgs& a)
 bool grad_roles_supported(const GradArgs& a)
 {
     if (!form_supported(a) || a.pb.D > 128) return false;
-    // Two load warps without asynchronous copies do not keep up with whole planes (odd widths: 1077 x 1080, D = 72: both gradients 686 us,
-    // 537 by the two kernels of sr_grad_tc.cu), nor with the dictionary's sums over gathered lists alone (1080p x4, s = 8: 473 / 303; both
-    // gradients 545 / 768; lists masked in place do: plan_fits).
-    const bool sums = a.gdict || a.ggamma;
-    if (sums && (a.mode == kModeDense || a.mode == kModeGlobal) && (a.pb.W % 2 != 0 || ((uintptr_t)a.coef & 3) != 0)) return false;
+    if (one_by_one(a) && grad_rows(a) < kPairsPlanes) return false;
     switch (a.pb.k) {
     case 3: return plan_fits<3>(a);
     case 5: return plan_fits<5>(a);

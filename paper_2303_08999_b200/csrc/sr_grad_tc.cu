@@ -1,5 +1,6 @@
 // Gradients of the dictionary regression on the tcgen05 tensor cores, for binary16 coefficients: k in {3, 5, 7}, up to four channels,
-// any width and number of atoms.
+// any width and number of atoms. For what the one kernel of sr_grad_roles.cu does not take: more than 128 atoms, operands that leave
+// it no room, odd widths with few planes.
 //
 //   grad_coef: per row of 128 pixels, a product [pixels x k*k][k*k x atoms]       (grad_coef_tc_kernel)
 //   grad_dict: per row of 128 pixels, a product [atoms x pixels][pixels x k*k]    (grad_dict_tc_kernel), summed over rows
@@ -305,7 +306,7 @@ grad_dict_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_consta
                     // (what a row put there is taken back by the thread that did, below)
                     const uint8_t* list = p.idx + (int64_t)w.f * s_ * HW + pix;
                     const __half* src = p.coef + (int64_t)w.f * p.planes * HW + pix;
-                    for (int q0 = 0; inside && q0 < s_; q0 += 8) {       // (eight loads in flight: one after the other took 250 us at 1080p, s = 8)
+                    for (int q0 = 0; inside && q0 < s_; q0 += 8) {       // (eight loads in flight)
                         int a[8];
                         __half h[8];
 #pragma unroll

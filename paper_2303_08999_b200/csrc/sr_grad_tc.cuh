@@ -74,10 +74,8 @@ __device__ __forceinline__ void tma_store_4d(const CUtensorMap* map, const void*
 }
 __device__ __forceinline__ void bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
 __device__ __forceinline__ void bulk_wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
-__device__ __forceinline__ void bulk_wait_read_but_one() { asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory"); }
 __device__ __forceinline__ void bulk_wait_all() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
-// Waits of a row's length (some hundred cycles): tested without the time hint of mbar_wait, whose sleep is longer than they are
-// (1080p x4, D = 72, k = 5: coefficients 137 -> 104 us, dictionary 129 -> 98). Bounded like it.
+// mbar_wait for waits of some hundred cycles: polls without suspending the thread. Bounded like it.
 __device__ __forceinline__ bool mbar_wait_short(uint64_t* bar, uint32_t parity, volatile WaitCtx* wc)
 {
     const uint32_t at = smem_u32(bar);
@@ -283,7 +281,7 @@ template <int K, int NG, bool NAMED> struct TileState {
 };
 
 // G of a pixel, times the tile's scale. `between` is called after the first channel. One and three channels are written out: a loop
-// over channels carries its k*k sums from register to register (293 instructions a row and warp for three, 5 x 5; 165 written out).
+// over channels carries its k*k sums from register to register (293 instructions a row and warp for three, 5 x 5).
 template <int K, int NC, typename Between>
 __device__ __forceinline__ void patch_grad_c(const float* u, int u_channel, const float* g, int C, float scale, float (&G)[K * K], Between between)
 {
