@@ -153,10 +153,12 @@ __device__ __forceinline__ bool load_barrier_and(int pair, bool ok)
 
 // ---- load warps ---------------------------------------------------------------------------------------------------------------
 
-// The bits of four pixels (0 .. 15) as two words of 16-bit masks: bit i to the sign of byte i, and the signs over the halves.
-__device__ __forceinline__ void mask_four(uint32_t b, uint32_t& m01, uint32_t& m23)
+// A word of bits covers 32 pixels; pixel 4 t + i stands at bit 8 i + 7 - t, so that a shift by t brings four neighbours to the signs of the
+// four bytes, and a permutation spreads those over 16-bit masks.
+__device__ __forceinline__ int bit_of_pixel(int px) { return 8 * (px & 3) + 7 - (px >> 2); }
+__device__ __forceinline__ void mask_four(uint32_t bits, int t, uint32_t& m01, uint32_t& m23)
 {
-    const uint32_t signs = b * 0x10204080u;
+    const uint32_t signs = bits << t;
     asm("prmt.b32 %0, %1, 0, 0x9988;" : "=r"(m01) : "r"(signs));
     asm("prmt.b32 %0, %1, 0, 0xBBAA;" : "=r"(m23) : "r"(signs));
 }
@@ -164,8 +166,8 @@ __device__ __forceinline__ void mask_four(uint32_t b, uint32_t& m01, uint32_t& m
 // Lists over whole planes: a row's planes land by TMA like those of the dense form, a warp takes 64 of its pixels, sets a bit for every
 // (atom, pixel) that a list names, and clears the values without one in place; the result warps read the same bits. All planes are read for
 // a few of each pixel's, but gathering those, two bytes at a time, waits for memory twice a row (1080p x4, D = 72, k = 5, s = 8: both
-// gradients 554 us, coefficients 287, dictionary 306; so 250, 166, 158). The instructions of a row's bits and masks are too many for one
-// pair of warps (335, 199, 286): three take a row each in turn.
+// gradients 554 us, coefficients 287, dictionary 306; so 247, 144, 162). The instructions of a row's bits and masks are too many for one
+// pair of warps (335, 199, 286): three take a row each in turn. (Four planes' loads before their first store: 300, 147, 212.)
 __device__ __forceinline__ void load_lists(const CUtensorMap* map, const RoleParams& p, RoleCtl& ctl, uint8_t* sPhi, uint8_t* sBits, int tid)
 {
     const Problem& pb = p.b.g.pb;
@@ -219,14 +221,14 @@ __device__ __forceinline__ void load_lists(const CUtensorMap* map, const RolePar
         for (int i = 0; i < 2; ++i) reinterpret_cast<uint4*>(bits)[lane + 32 * i] = make_uint4(0u, 0u, 0u, 0u);
         __syncwarp();
         uint32_t* word = bits + (px >> 5) * 128;
-        const uint32_t first = x0 + 64 * warp + px < pb.W ? 1u << (px & 31) : 0u;
+        const uint32_t first = x0 + 64 * warp + px < pb.W ? 1u << bit_of_pixel(px & 31) : 0u;            // (px is the first of four: the others' are 8, 16, 24 higher)
         for (int q0 = 0;; ) {
 #pragma unroll
             for (int i = 0; i < 8; ++i)
                 if (q0 + 2 * i < s) {
                     const uint32_t bit = q0 + 2 * i + odd < s ? first : 0u;
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) atomicOr(word + min((int)(a[i] >> (8 * j) & 255u), pb.D - 1), bit << j);
+                    for (int j = 0; j < 4; ++j) atomicOr(word + min((int)(a[i] >> (8 * j) & 255u), pb.D - 1), bit << (8 * j));
                 }
             if ((q0 += 16) >= s) break;
             ask(x0, y, f, q0);
@@ -245,12 +247,12 @@ __device__ __forceinline__ void load_lists(const CUtensorMap* map, const RolePar
         const int unit = lane & 7;
 #pragma unroll 4
         for (int l = lane >> 3; l < pb.D; l += 4) {
-            const uint32_t b = reinterpret_cast<const uint8_t*>(bits)[(unit >> 2) * 512 + l * 4 + (unit & 3)];
+            const uint32_t b = bits[(unit >> 2) * 128 + l];
             uint4* at = reinterpret_cast<uint4*>(chunk + l * 128 + ((unit ^ (l & 7)) << 4));
             uint4 v = *at;
             uint32_t m0, m1, m2, m3;
-            mask_four(b & 15u, m0, m1);
-            mask_four(b >> 4, m2, m3);
+            mask_four(b, 2 * (unit & 3), m0, m1);
+            mask_four(b, 2 * (unit & 3) + 1, m2, m3);
             *at = make_uint4(v.x & m0, v.y & m1, v.z & m2, v.w & m3);
         }
         fence_proxy_async_smem();
@@ -449,6 +451,7 @@ template <int K, Form FORM> __device__ __forceinline__ void result_role(const CU
     const int64_t HW = (int64_t)pb.H * W;
     const uint32_t at = tmem + ((uint32_t)(32 * warp) << 16), acc_at = at + grp * 128;
     constexpr int STEP = K == 7 ? 16 : 32;                   // accumulator columns at a time (registers)
+    constexpr int kUnroll = FORM == kLists ? 1 : 2;          // (lists: less code for more roles; coefficients of lists 170 -> 144 us with the shorter masks)
     constexpr bool any = FORM == kGeneral || FORM == kPairs;
     const bool listed = any && p.b.mode == kModeIdx, compact = any && p.b.mode == kModeCompact;
     const bool together = p.want_coef && (listed || compact);        // these meet at barriers, so they leave together
@@ -475,7 +478,7 @@ template <int K, Form FORM> __device__ __forceinline__ void result_role(const CU
                 if (tl.x0 + tid < W)
                     for (int q = 0; q < pb.s; ++q) {
                         const int a = min((int)__ldg(p.b.idx + ((int64_t)tl.f * pb.s + q) * HW + pix + tid), pb.D - 1);
-                        atomicOr(&ctl.listed[grp][a][tid >> 5], 1u << (tid & 31));
+                        atomicOr(&ctl.listed[grp][a][tid >> 5], 1u << bit_of_pixel(tid & 31));
                     }
             }
             if (FORM == kLists) {
@@ -494,7 +497,7 @@ template <int K, Form FORM> __device__ __forceinline__ void result_role(const CU
             }
             tc_fence_after_sync();
             const float k = back * *(volatile float*)&ctl.unscale[tl.n % kUnscales];
-#pragma unroll
+#pragma unroll kUnroll
             for (int c0 = 0; c0 < 128; c0 += 64) {
                 if (compact) {
                     if (!(ok = result_barrier(ok))) break;   // the chunk before has been taken
@@ -523,10 +526,10 @@ template <int K, Form FORM> __device__ __forceinline__ void result_role(const CU
                                 h[i] = *reinterpret_cast<const uint32_t*>(&v2) & whole;      // (an atom outside the subset: zeros, whatever G is)
                             }
                             if (listed || FORM == kLists) {  // pixels that do not list the atom
-                                const uint32_t b = keep[(c0 + c1 + 8 * j) / 32] >> ((c0 + c1 + 8 * j) % 32);
+                                const uint32_t b = (c1 + 8 * j) / 32 ? (c0 ? keep[3] : keep[1]) : (c0 ? keep[2] : keep[0]);
                                 uint32_t m[4];
-                                mask_four(b & 15u, m[0], m[1]);
-                                mask_four(b >> 4 & 15u, m[2], m[3]);
+                                mask_four(b, (c1 + 8 * j) % 32 / 4, m[0], m[1]);
+                                mask_four(b, (c1 + 8 * j) % 32 / 4 + 1, m[2], m[3]);
 #pragma unroll
                                 for (int i = 0; i < 4; ++i) h[i] &= m[i];
                             }
