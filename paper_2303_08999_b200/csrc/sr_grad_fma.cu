@@ -486,7 +486,9 @@ template <int K, typename CoefT> cudaError_t launch_dict_t(const GradArgs& a, in
     if (cudaError_t e = raise_smem(kern, smem)) return e;
     count_launches(1);
     *slots = gx;
-    return launch_after_smem(kern, dim3(gx, (p.rows + p.chunk - 1) / p.chunk), 256, smem, a.st, p, static_cast<const CoefT*>(a.coef));
+    // Early only behind this call's own coefficient kernel, which started after everything before the call; behind another kernel this one
+    // would read inputs that are still being written, if that one lets the next launch start.
+    return launch_after_smem(kern, dim3(gx, (p.rows + p.chunk - 1) / p.chunk), 256, smem, a.st, a.gcoef != nullptr, p, static_cast<const CoefT*>(a.coef));
 }
 
 template <typename CoefT> cudaError_t launch_coef_k(const GradArgs& a)

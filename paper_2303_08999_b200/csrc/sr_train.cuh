@@ -72,8 +72,9 @@ cudaError_t launch_adamw(const sr_adamw_tensor* tensors, int count, int param_dt
 #ifdef __CUDACC__
 // A kernel that sums what the launch before it on the stream wrote: it may be brought up while that one ends (programmatic dependent
 // launch) and waits for its end, with all it wrote, in wait_for_launch_before().
+// (early = false: an ordinary launch, for a kernel that reads what came before the call without waiting.)
 template <typename... Params, typename... Args>
-cudaError_t launch_after_smem(void (*kern)(Params...), dim3 grid, int threads, size_t smem, cudaStream_t st, Args... args)
+cudaError_t launch_after_smem(void (*kern)(Params...), dim3 grid, int threads, size_t smem, cudaStream_t st, bool early, Args... args)
 {
     cudaLaunchAttribute attr{};
     attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -84,13 +85,13 @@ cudaError_t launch_after_smem(void (*kern)(Params...), dim3 grid, int threads, s
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
     cfg.attrs = &attr;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = early ? 1 : 0;
     return cudaLaunchKernelEx(&cfg, kern, static_cast<Params>(args)...);
 }
 template <typename... Params, typename... Args>
 cudaError_t launch_after(void (*kern)(Params...), dim3 grid, int threads, cudaStream_t st, Args... args)
 {
-    return launch_after_smem(kern, grid, threads, 0, st, args...);
+    return launch_after_smem(kern, grid, threads, 0, st, true, args...);
 }
 
 // In the launch before: the next one may be brought up now, beside this one (one that depends on nothing this one writes).

@@ -104,6 +104,20 @@ def test_selected(n, c, h, w, r, D, k, s, dt, mode):
     assert sr.sr_device_status() == 0
 
 
+@pytest.mark.parametrize("k", [3, 5, 7])
+@pytest.mark.parametrize("n,h,w", [(1, 1, 8), (1, 2, 8), (2, 3, 16), (1, 1, 136), (3, 5, 136), (1, 17, 120)])
+def test_lists_on_frames_with_fewer_rows_than_a_tile(n, h, w, k):
+    lr, coef, d, g = _inputs(n, 3, h, w, 1, 9, k, "f16", seed=h + w)
+    idx, coef = _select(coef, 2, False)
+    want, mags = train_ref.grads(lr, coef, idx, None, d, g, 1, k, "listed")
+    for kw in ({}, {"want_dict": False}, {"want_coef": False}):
+        got = sr.sr_dict_regress_selected_grad(to(lr), to(coef), to(idx), None, to(d), to(g), 1, k, 2, **kw)
+        have = [i for i in (0, 1) if got[i] is not None]
+        full = sr.sr_dict_regress_selected_grad(to(lr), to(coef), to(idx), None, to(d), to(g), 1, k, 2)
+        _check([got[i] if i in have else full[i] for i in (0, 1)] + [None], want, mags, 3, k, "f16", n * h * w)
+    assert sr.sr_device_status() == 0
+
+
 def test_subset_without_reweights_in_any_order_and_with_an_atom_twice():
     lr, coef, d, g = _inputs(1, 3, 16, 24, 2, 24, 5, "f16", seed=4)
     for idx, gamma in (([9, 3, 17], None), ([5, 2, 5, 11], [0.5, 1.5, -2.0, 1.0]), ([7], [0.0])):
@@ -399,6 +413,23 @@ def test_a_wait_that_runs_out_is_reported_and_the_next_call_is_clean(case):
         sr.sr_test_lose_arrival(0)
         sr.sr_set_wait_limit(old)
     assert all(torch.equal(a, b) for a, b in zip(call(), before)) and sr.sr_device_status() == 0
+
+
+@pytest.mark.parametrize("dt", ["f32", "f16"])
+@pytest.mark.parametrize("D,k", [(72, 5), (24, 9)])
+def test_a_call_that_reads_what_the_call_before_it_writes(dt, D, k):
+    """The dictionary's gradient alone, for coefficients that the call before on the stream is still writing (another call's grad_coef)."""
+    lr, coef, d, g = (to(a) for a in _inputs(2, 3, 90, 120, 4, D, k, dt, seed=17))
+    made, first = torch.empty_like(coef), None
+    for wait in (True, False, False, False):
+        made.zero_()
+        torch.cuda.synchronize()
+        sr.sr_dict_regress_dense_grad(lr, coef, d, g, 4, k, grad_coef=made, want_dict=False)
+        if wait:
+            torch.cuda.synchronize()
+        gd = sr.sr_dict_regress_dense_grad(lr, made, d, g, 4, k, want_coef=False)[1]
+        first = gd.clone() if first is None else first
+        assert torch.equal(gd, first)
 
 
 def test_two_calls_at_once_with_a_scratch_each():
