@@ -390,8 +390,9 @@ int sr_select_balance_grad(const void* coef, int coef_dtype, const uint8_t* mask
  *   state_bits = 32: m, v are fp32 [n]; the scale pointers are ignored.
  *   state_bits = 8:  m and v are one byte an element, e4m3, with one fp32 scale for each 256 consecutive elements (the last
  *                    block may be shorter): m = m_scale * code, sqrt(v) = v_scale * code.  After the step a block's scale is its
- *                    largest magnitude / 448 and codes are rounded to nearest even; a root that is not zero is not held as zero
- *                    (the step would divide by it).  All-zero codes and scales are a fresh state.
+ *                    largest magnitude times 1/448 and a code is value / scale, rounded to nearest even; a root that is not zero is
+ *                    not held as zero (the step would divide by it).  Codes and scales are those of the formulas above with every
+ *                    operation (and 1/448) rounded to fp32.  All-zero codes and scales are a fresh state.
  * A tensor of n = 0 elements is skipped (its pointers may be NULL); tensors of one call must not overlap.
  * opts (HOST): lr_dev (fp32 [1]), step_dev (int64 [1]) and skip_dev (int32 [1]) are device pointers or NULL; the first two replace lr
  * and step and the third, where it is not 0, makes the call change nothing, so that a captured step can be replayed with a
