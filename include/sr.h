@@ -397,7 +397,7 @@ int sr_select_balance_grad(const void* coef, int coef_dtype, const uint8_t* mask
  * opts (HOST): lr_dev (fp32 [1]), step_dev (int64 [1]) and skip_dev (int32 [1]) are device pointers or NULL; the first two replace lr
  * and step and the third, where it is not 0, makes the call change nothing, so that a captured step can be replayed with a
  * schedule, a counter the caller advances, and a found-Inf flag.  A gradient that is not finite gives a parameter and state that
- * are not finite (8 bits: for its whole block): skip such steps.  The paper names no optimiser; AdamW is the common choice.
+ * are not finite (8 bits: the state of its whole block, by its scales): skip such steps.  The paper names no optimiser; AdamW is the common choice.
  */
 typedef struct sr_adamw_tensor {
     void* param;

@@ -117,7 +117,7 @@ __device__ __forceinline__ void over_scale(float (&out)[8], const float (&v)[8],
 
 // A parameter's step takes division, and with 32-bit states the root, at the speed of their approximate instructions (2 and 1 units in the
 // last place of the step, which is small beside the parameter). Exact ones, 63 M parameters: fp32 262 us both ways; 16-bit parameters
-// and gradients 207 -> 229; 8-bit states 195 -> 207; three small tensors 9.2 -> 11.3. The 8-bit states' root is exact: it is stored.
+// and gradients 207 -> 229; 8-bit states 12 more; three small tensors 9.2 -> 11.3. The 8-bit states' root is exact: it is stored.
 __device__ __forceinline__ float fast_sqrt(float v)
 {
     float r;
@@ -125,10 +125,17 @@ __device__ __forceinline__ float fast_sqrt(float v)
     return r;
 }
 
+// The larger one, NaN where either is: a block with a value that is not finite has a scale that is not, and so no state that looks valid.
+__device__ __forceinline__ float max_or_nan(float a, float b)
+{
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
 __device__ __forceinline__ float warp_max(float v)
 {
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
+    for (int o = 16; o > 0; o >>= 1) v = max_or_nan(v, __shfl_xor_sync(0xffffffffu, v, o));
     return v;
 }
 
@@ -195,7 +202,7 @@ adamw_kernel(const __grid_constant__ AdamwList<N> list, const __grid_constant__ 
         const float gi = g[i] * o.grad_scale;
         if (BITS == 8) {
             // Every operation rounded by itself: where a sum is contracted, a value next to the middle of two codes goes to the other one
-            // (8 of 5 M). With the exact root and quotients: 63 M parameters 173 -> 195 us.
+            // (8 of 5 M). With the exact root and quotients: 63 M parameters 174 -> 188 us.
             m[i] = __fadd_rn(__fmul_rn(o.beta1, m[i]), __fmul_rn(o.one_beta1, gi));
             v[i] = __fadd_rn(__fmul_rn(o.beta2, v[i]), __fmul_rn(o.one_beta2, __fmul_rn(gi, gi)));
             root[i] = __fsqrt_rn(v[i]);
@@ -214,7 +221,7 @@ adamw_kernel(const __grid_constant__ AdamwList<N> list, const __grid_constant__ 
         float top_m = 0.f, top_v = 0.f;
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-            if (i < have) { top_m = fmaxf(top_m, fabsf(m[i])); top_v = fmaxf(top_v, root[i]); }
+            if (i < have) { top_m = max_or_nan(top_m, fabsf(m[i])); top_v = max_or_nan(top_v, root[i]); }
         const float sm = warp_max(top_m) * kPerF8Max, sv = warp_max(top_v) * kPerF8Max;
         alignas(8) uint8_t a[8], b[8];
         float q[8];

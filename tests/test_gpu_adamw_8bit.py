@@ -87,3 +87,34 @@ def test_values_half_way_between_two_codes(unit):
     sr.sr_adamw_step(sr.sr_adamw_plan([torch.zeros_like(g)], *state, *scales), [g], 1, 1e-3, 0.0, 0.9)
     _same((state[0][0], scales[0][0], state[1][0], scales[1][0]),
           _step(g, *(torch.zeros_like(y[0]) for y in state + scales), 0.0, 0.9, 1.0), g.numel())
+
+
+@pytest.mark.parametrize("gtype", [torch.float32, torch.float16])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
+@pytest.mark.parametrize("n,at,rest", [(1, [0], 0.0), (256, [17], 0.0), (256, [255], 0.5), (256, range(256), 0.0), (300, [299], 0.25), (300, [3], 0.0), (1000, [256, 511], 1.0)])
+def test_a_gradient_that_is_not_finite_marks_its_whole_block(n, at, rest, bad, gtype):
+    """None of the block's states is finite after the step or after a clean one; the other blocks are those of a step without it."""
+    at = list(at)
+    hit = torch.zeros((n + BLOCK - 1) // BLOCK, dtype=torch.bool, device="cuda")
+    hit[[i // BLOCK for i in at]] = True
+    element = hit.repeat_interleave(BLOCK)[:n]
+    runs = []
+    for value in (0.125, bad):                           # the same run without and with it
+        p = [torch.ones(n, device="cuda")]
+        state, scale = _fresh([n])
+        plan = sr.sr_adamw_plan(p, *state, *scale)
+        sr.sr_adamw_step(plan, [torch.full((n,), 0.5, device="cuda", dtype=gtype)], 1, 1e-3)
+        g = torch.full((n,), rest, device="cuda", dtype=gtype)
+        g[at] = value
+        sr.sr_adamw_step(plan, [g], 2, 1e-3)
+        runs.append([p[0].clone(), *(c[0].float() * s[0].repeat_interleave(BLOCK)[:n] for c, s in zip(state, scale))])
+        sr.sr_adamw_step(plan, [torch.full((n,), 0.5, device="cuda", dtype=gtype)], 3, 1e-3)
+        runs[-1] += [p[0], *(c[0].float() * s[0].repeat_interleave(BLOCK)[:n] for c, s in zip(state, scale))]
+    clean, got = runs
+    for i in (1, 2, 4, 5):                               # the moments after the step and after the next
+        assert not torch.isfinite(got[i][element]).any()
+        assert torch.equal(got[i][~element], clean[i][~element])
+    assert not torch.isfinite(got[0][at]).any() and not torch.isfinite(got[3][element]).any()
+    others = torch.ones(n, dtype=torch.bool, device="cuda")
+    others[at] = False
+    assert torch.equal(got[0][others], clean[0][others]) and torch.equal(got[3][~element], clean[3][~element])
