@@ -68,6 +68,21 @@ cudaError_t launch_select(const void* coef, int coef_dtype, uint8_t* idx, void* 
 cudaError_t launch_luma_lr(const float* lr_frame, float* ylr, const Problem& pb, cudaStream_t st);
 cudaError_t launch_luma_combine(const float* lr_frame, float* out_frame, const Problem& pb, cudaStream_t st);
 
+// Allows `kern` `most` bytes of dynamic shared memory, once a device (`done`: a static of the kernel's launcher). The most that any of its
+// calls takes, not this call's size: the limit belongs to the kernel, so a smaller call of another thread would lower it between a
+// call's setting and its launch.
+template <typename Kern> inline cudaError_t allow_most_smem(Kern kern, size_t most, bool (&done)[64])
+{
+    int dev = 0;
+    if (cudaError_t e = cudaGetDevice(&dev)) return e;
+    if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
+    if (!done[dev]) {
+        if (cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)most)) return e;
+        done[dev] = true;
+    }
+    return cudaSuccess;
+}
+
 // ---- device helpers ------------------------------------------------------------------------------------------------
 
 __device__ __forceinline__ int clampi(int v, int lo, int hi) { return min(max(v, lo), hi); }

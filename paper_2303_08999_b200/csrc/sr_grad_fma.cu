@@ -437,12 +437,6 @@ grad_subset_sum_kernel(const float* __restrict__ partial, int slots, int s, int 
     if (first && gdict && tid < kk) gdict[(int64_t)atom * kk + tid] = (float)rowsum[tid];
 }
 
-template <typename Kern> cudaError_t raise_smem(Kern kern, size_t smem)
-{
-    // (48 KB hold without being asked for: what is dynamic and the kernels' ten static KB)
-    return smem > 36 * 1024 ? cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) : cudaSuccess;
-}
-
 template <int K, typename CoefT> cudaError_t launch_coef_t(const GradArgs& a)
 {
     constexpr int TY = 8;
@@ -454,7 +448,9 @@ template <int K, typename CoefT> cudaError_t launch_coef_t(const GradArgs& a)
     const int blocks = (int)(tiles < 4 * sm_count() ? tiles : 4 * sm_count());
     const size_t smem = (size_t)pb.D * KK<K>::padded * sizeof(float) + sizeof(UTile<K, TY>);
     auto kern = grad_coef_kernel<K, CoefT>;
-    if (cudaError_t e = raise_smem(kern, smem)) return e;
+    constexpr size_t most = 256 * KK<K>::padded * sizeof(float) + sizeof(UTile<K, TY>);        // 256 atoms
+    static bool done[64] = {false};
+    if (cudaError_t e = allow_most_smem(kern, most, done)) return e;
     kern<<<blocks, dim3(TX, TY), smem, a.st>>>(p, static_cast<CoefT*>(a.gcoef));
     count_launches(1);
     return cudaGetLastError();
@@ -483,7 +479,10 @@ template <int K, typename CoefT> cudaError_t launch_dict_t(const GradArgs& a, in
     const size_t sums = (size_t)((p.chunk + 3) / 4) * TG * 16 * sizeof(float);
     if (smem < sums) smem = sums;
     auto kern = grad_dict_kernel<K, CoefT>;
-    if (cudaError_t e = raise_smem(kern, smem)) return e;
+    constexpr size_t planes = (kMost + 3) & ~3, most_sums = planes / 4 * TG * 16 * sizeof(float);
+    constexpr size_t most_tiles = (KK<K>::padded + planes * 2) * PITCH * sizeof(float) + sizeof(UTile<K, TY>), most = most_tiles > most_sums ? most_tiles : most_sums;
+    static bool done[64] = {false};
+    if (cudaError_t e = allow_most_smem(kern, most, done)) return e;
     count_launches(1);
     *slots = gx;
     // Early only behind this call's own coefficient kernel, which started after everything before the call; behind another kernel this one
