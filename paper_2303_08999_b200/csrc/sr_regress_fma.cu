@@ -189,12 +189,11 @@ cudaError_t launch_t(const float* lr, const void* coef, const uint8_t* idx, cons
                      float* out, const Problem& pb, cudaStream_t st)
 {
     constexpr int P = (K - 1) / 2;
-    const size_t smem = ((size_t)pb.D * KK<K>::padded + (size_t)CCHUNK * (TY + 2 * P) * (TX + 2 * P)) * sizeof(float);
+    constexpr size_t tile = (size_t)CCHUNK * (TY + 2 * P) * (TX + 2 * P) * sizeof(float), atom = KK<K>::padded * sizeof(float);
+    const size_t smem = pb.D * atom + tile;
     auto kern = regress_fma_kernel<K, CoefT, MODE>;
-    if (smem > 48 * 1024) {
-        cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-        if (e != cudaSuccess) return e;
-    }
+    static bool done[64] = {false};
+    if (cudaError_t e = allow_most_smem(kern, 256 * atom + tile, done)) return e;
     dim3 grid((pb.W + TX - 1) / TX, (pb.H + TY - 1) / TY, pb.n), block(TX, TY);
     if (grid.y > 65535 || grid.z > 65535) return cudaErrorInvalidConfiguration;
     kern<<<grid, block, smem, st>>>(lr, (const CoefT*)coef, idx, gamma, dict, out, pb);

@@ -7,6 +7,7 @@ import pytest
 import torch
 
 import paper_2303_08999_b200 as sr
+from gpu_util import on_kernel
 from paper_2303_08999_b200 import api
 
 pytestmark = pytest.mark.gpu
@@ -52,3 +53,19 @@ def test_fp32_gradients_of_different_sizes(k, sizes):
     torch.cuda.synchronize()
     assert _at_once(jobs, 4000) == []
     assert all(torch.equal(x, y) for want, got in outs for x, y in zip(want, got))
+
+
+def test_general_regressions_of_different_sizes():
+    """9 x 9 atoms, whose dictionary is the largest that the general kernel holds: 160 to 256 atoms, a size of shared memory each."""
+    lib, jobs, outs = sr.load_library(), [], []
+    with on_kernel(0):
+        for D in (160, 200, 240, 256):
+            lr, coef, d, _, dims = _problem(D, 9)
+            want = sr.sr_dict_regress_dense(lr, coef, d, 1, 9)
+            out = torch.empty_like(want)
+            outs.append((want, out))
+            jobs.append(lambda st, a=(lr, coef, d, out), dims=dims: lib.sr_dict_regress_dense(
+                a[0].data_ptr(), a[1].data_ptr(), api.SR_F32, a[2].data_ptr(), a[3].data_ptr(), ctypes.byref(dims), 0, st))
+        torch.cuda.synchronize()
+        assert _at_once(jobs, 4000) == []
+    assert all(torch.equal(want, got) for want, got in outs)
