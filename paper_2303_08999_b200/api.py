@@ -561,8 +561,8 @@ _ADAMW_CODES = {torch.float32: SR_F32, torch.float16: SR_F16, torch.bfloat16: SR
 
 class AdamwPlan:
     """The tensors of sr_adamw_step, checked once and laid out for the call. A parameter whose storage was replaced (p.data = ...) is
-    followed: every step reads the parameters' addresses afresh. The states belong to the plan while it lives: change them in place,
-    or make a new plan (it keeps their memory, so a state that was given other storage is not followed but stays valid)."""
+    followed: every step reads the parameters' addresses and sizes afresh. The states belong to the plan while it lives: change them in
+    place, or make a new plan (it keeps their memory, so a state that was given other storage is not followed but stays valid)."""
 
     def __init__(self, params, exp_avg, exp_avg_sq, avg_scale=None, avg_sq_scale=None):
         self.params, self.m, self.v = list(params), list(exp_avg), list(exp_avg_sq)
@@ -604,15 +604,21 @@ class AdamwPlan:
         if self.params[i].device != self.device:
             raise ValueError("all tensors of a plan must be on one device")
 
-    def _follow(self, at):
-        """Parameters whose address is another than at the last step."""
-        for i, (a, b) in enumerate(zip(at, self._at)):
-            if a != b:
-                self._check(i)
-        if [p.numel() for p in self.params] != self._sizes:
+    def _follow(self):
+        """The parameters as they are now. The address alone does not tell: another view of the old memory, or new memory where the old was
+        freed, may have it."""
+        tensor = torch.Tensor
+        at = list(map(tensor.data_ptr, self.params))
+        if list(map(tensor.numel, self.params)) != self._sizes:
             raise ValueError("a parameter changed its size: make a new plan")
-        self._at = at
-        self._columns[:, 0] = at
+        if not all(map(tensor.is_contiguous, self.params)) or {p.dtype for p in self.params} != {self.param_dtype}:
+            raise TypeError(f"a parameter is not a contiguous tensor of {self.param_dtype} any more: make a new plan")
+        if at != self._at:
+            for i, (a, b) in enumerate(zip(at, self._at)):
+                if a != b:
+                    self._check(i)
+            self._at = at
+            self._columns[:, 0] = at
 
 
 def sr_adamw_plan(params, exp_avg, exp_avg_sq, avg_scale=None, avg_sq_scale=None) -> AdamwPlan:
@@ -638,9 +644,7 @@ def sr_adamw_step(plan: AdamwPlan, grads, step, lr, beta1: float = 0.9, beta2: f
             not all(map(tensor.is_contiguous, grads)) or list(map(tensor.numel, grads)) != plan._sizes:
         raise TypeError(f"grads must be contiguous {dtype} tensors on {plan.device}, of their parameters' sizes")
     plan._columns[:, 1] = list(map(tensor.data_ptr, grads))
-    at = list(map(tensor.data_ptr, plan.params))
-    if at != plan._at:
-        plan._follow(at)
+    plan._follow()
     o = sr_adamw_opts(0.0, beta1, beta2, eps, weight_decay, grad_scale, 1, None, None, None)
     for value, dev_type, host, dev in ((lr, torch.float32, "lr", "lr_dev"), (step, torch.int64, "step", "step_dev"), (skip, torch.int32, None, "skip_dev")):
         if isinstance(value, torch.Tensor):
