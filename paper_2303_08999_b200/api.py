@@ -436,8 +436,13 @@ def _same_device(first, **others):
             raise ValueError(f"{what} is on {t.device}, lr or coef on {first.device}")
 
 
+# The kernels write through addresses, which autograd does not see: what a caller's tensor is written for is said here, so that a backward
+# pass which saved it refuses as it does after PyTorch's own changes in place.
+_changed_in_place = torch.autograd.graph.increment_version
+
+
 def _grad_out_of(t, shape, dtype, want: bool, like, what: str):
-    """A gradient's buffer: None when it is not wanted, `t` checked, or a new tensor."""
+    """A gradient's buffer: None when it is not wanted, `t` checked (and counted as changed), or a new tensor."""
     if not want:
         return None
     if t is None:
@@ -445,6 +450,7 @@ def _grad_out_of(t, shape, dtype, want: bool, like, what: str):
     _dev(t, dtype, what)
     if t.shape != shape:
         raise ValueError(f"{what} must be {tuple(shape)}")
+    _changed_in_place(t)
     return t
 
 
@@ -655,5 +661,6 @@ def sr_adamw_step(plan: AdamwPlan, grads, step, lr, beta1: float = 0.9, beta2: f
             setattr(o, host, value)
         elif value is not None:
             raise TypeError("skip must be an int32 CUDA tensor")
+    _changed_in_place(plan.params)
     _check((_lib or load_library()).sr_adamw_step(table, len(grads), _ADAMW_CODES[plan.param_dtype], _ADAMW_CODES[dtype], plan.state_bits,
                                                   ctypes.byref(o), _stream()), "sr_adamw_step")
