@@ -367,6 +367,7 @@ int sr_dict_regress_selected_grad(const float* lr, const void* coef_or_sel, int 
  * zero for pixels that do not count or whose sum is below the smallest normal number; counts have no gradient.  grad_loss: device
  * fp32 [1] or NULL (1).  SR_GRAD_ADD adds it to grad_coef (read and rounded in the coefficient dtype; a pixel that does not count keeps
  * its bits), e.g. to what the regression's gradient wrote.  The values are of the order weight / T: with binary16 use a loss scale.
+ * Sums so small that weight * slope * sum leaves the normal fp32 numbers cost bits of the mean slope.
  * A valid pixel with a coefficient that is not finite, or whose sum overflows fp32, has an unspecified gradient, and makes share, loss
  * and slope-weighted results of its frame unspecified.  grad_coef must not overlap coef.
  *

@@ -376,7 +376,7 @@ template <bool ADD> __device__ __forceinline__ uint32_t result_word(const __half
 }
 
 // Atoms whose gradient to add to is in flight: all of a warp's where the registers allow (binary16, 1080p, D = 72: 201 us with four and
-// three blocks a multiprocessor, 160 with all nine and two; fp32: 317 with four and three blocks, 371 with nine and two).
+// three blocks a multiprocessor, 160 with all nine and two; fp32: 317 with four and three blocks, 371 with nine and two; all with the slopes in registers).
 template <typename CoefT, int AW> __host__ __device__ constexpr int ahead_of() { return Lane<CoefT>::PER == 2 && AW <= 9 ? AW : 4; }
 
 template <typename CoefT, int AW, int WARPS, bool VEC, bool ADD>
@@ -387,8 +387,9 @@ balance_grad_kernel(const CoefT* __restrict__ coef, CoefT* __restrict__ grad, co
     constexpr int PER = L::PER, PX = NW * PER, TP = 32 * PX;
     __shared__ __align__(16) float ssum[WARPS][TP];
     __shared__ __align__(16) float sdot[WARPS][TP];
-    __shared__ __align__(16) float sk[TP];                       // weight / S
-    __shared__ __align__(16) float sc[TP];                       // - mean slope * weight / S
+    __shared__ float sa[AW * WARPS];                             // weighted slopes
+    __shared__ __align__(16) float sk[TP];                       // 1 / S, 0 for a pixel that does not count
+    __shared__ __align__(16) float sc[TP];                       // - mean weighted slope / S
     const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
     const int f = blockIdx.x / p.tiles;
     const int64_t p0 = (int64_t)(blockIdx.x - f * p.tiles) * TP;
@@ -399,14 +400,20 @@ balance_grad_kernel(const CoefT* __restrict__ coef, CoefT* __restrict__ grad, co
     uint32_t x[AW][NW], keep[NW];
     load_words<CoefT, AW, WARPS, VEC>(x, coef + (int64_t)f * D * HW + p0, HW, left, D, warp, lane);
     keep_words<CoefT, VEC>(keep, tile_mask, left, lane);
-    float a[AW];
-#pragma unroll
-    for (int j = 0; j < AW; ++j) a[j] = warp + j * WARPS < D ? __ldg(p.slope + (int64_t)f * D + warp + j * WARPS) : 0.f;
+    // The weight goes into the slopes, not into 1 / S: weight / S is beyond fp32 for small S where the gradient, which has a slope's
+    // size (about 1 / pixels) in it too, is not. In shared memory they leave the registers to the planes (1080p, D = 72, added: binary16
+    // 160 -> 149 us, fp32 362 -> 299; written 100 -> 104, 192 both).
+    if (tid < AW * WARPS) {
+        const float weight = p.grad_loss ? p.weight * __ldg(p.grad_loss) : p.weight;
+        sa[tid] = tid < D ? weight * __ldg(p.slope + (int64_t)f * D + tid) : 0.f;
+    }
+    __syncthreads();
     float sum[PX], dot[PX];
 #pragma unroll
     for (int i = 0; i < PX; ++i) sum[i] = dot[i] = 0.f;
 #pragma unroll
     for (int j = 0; j < AW; ++j) {
+        const float a = sa[warp + j * WARPS];
         uint32_t m[NW];
 #pragma unroll
         for (int w = 0; w < NW; ++w) m[w] = x[j][w] & keep[w];
@@ -414,7 +421,7 @@ balance_grad_kernel(const CoefT* __restrict__ coef, CoefT* __restrict__ grad, co
         for (int i = 0; i < PX; ++i) {
             const float v = L::get(m, i);
             sum[i] += v;
-            dot[i] = fmaf(a[j], v, dot[i]);
+            dot[i] = fmaf(a, v, dot[i]);
         }
     }
     CoefT* dst = grad + ((int64_t)f * D + warp) * HW + p0 + (VEC ? lane * PX : lane);
@@ -435,11 +442,10 @@ balance_grad_kernel(const CoefT* __restrict__ coef, CoefT* __restrict__ grad, co
         float S = 0.f, Q = 0.f;
 #pragma unroll
         for (int w = 0; w < WARPS; ++w) { S += ssum[w][tid]; Q += sdot[w][tid]; }
-        const float weight = p.grad_loss ? p.weight * __ldg(p.grad_loss) : p.weight;
         const bool on = tid < left && !(S < kSmallestNormal) && (!tile_mask || __ldg(tile_mask + tid) != 0);
-        const float r = 1.f / S, k = on ? weight * r : 0.f;
-        sk[tid] = k;
-        sc[tid] = on ? -(Q * r) * k : 0.f;
+        const float r = 1.f / S;
+        sk[tid] = on ? r : 0.f;
+        sc[tid] = on ? -(Q * r) * r : 0.f;
     }
     __syncthreads();
     float k[PX], c[PX];
@@ -456,6 +462,7 @@ balance_grad_kernel(const CoefT* __restrict__ coef, CoefT* __restrict__ grad, co
     for (int j = 0; j < AW; ++j) {
         if (warp + j * WARPS >= D) break;
         CoefT* to = dst + (int64_t)j * WARPS * HW;
+        const float a = sa[warp + j * WARPS];
         uint32_t old[NW], o[NW];
 #pragma unroll
         for (int w = 0; w < NW; ++w) old[w] = 0u;
@@ -472,7 +479,7 @@ balance_grad_kernel(const CoefT* __restrict__ coef, CoefT* __restrict__ grad, co
         for (int w = 0; w < NW; ++w) {
             float d[PER];
 #pragma unroll
-            for (int i = 0; i < PER; ++i) d[i] = fmaf(a[j], k[w * PER + i], c[w * PER + i]);
+            for (int i = 0; i < PER; ++i) d[i] = fmaf(a, k[w * PER + i], c[w * PER + i]);
             o[w] = result_word<ADD>((const CoefT*)nullptr, x[j][w], old[w], d);
             if (ADD && !decltype(every)::value) {                   // a pixel that does not count keeps its bits
 #pragma unroll
