@@ -436,6 +436,22 @@ def _same_device(first, **others):
             raise ValueError(f"{what} is on {t.device}, lr or coef on {first.device}")
 
 
+def _span(t):
+    at = t.data_ptr()
+    return at, at + t.numel() * t.element_size()
+
+
+def _apart(written: dict, read: tuple) -> None:
+    """The caller's tensors that a call writes share no memory with each other or with what it reads. (New ones never do.)"""
+    spans = [(*_span(t), what) for what, t in written.items() if t is not None]
+    if not spans:
+        return
+    others = [_span(t) for t in read if t is not None]
+    for i, (a, b, what) in enumerate(spans):
+        if any(a < d and c < b for c, d in others) or any(a < d and c < b for c, d, _ in spans[:i]):
+            raise ValueError(f"{what} shares memory with another tensor of the call")
+
+
 # The kernels write through addresses, which autograd does not see: what a caller's tensor is written for is said here, so that a backward
 # pass which saved it refuses as it does after PyTorch's own changes in place.
 _changed_in_place = torch.autograd.graph.increment_version
@@ -467,6 +483,7 @@ def sr_dict_regress_dense_grad(lr, coef, dict_, grad_out, scale: int, k: int, fl
     if dict_.shape != (D, k * k) or coef.shape != (n, D, H, W) or grad_out.shape != (n, c, H, W):
         raise ValueError("shapes of lr / coef / dict / grad_out do not agree")
     _same_device(lr, coef=coef, dict=dict_, grad_out=grad_out, grad_coef=grad_coef, grad_dict=grad_dict, scratch=scratch)
+    _apart({"grad_coef": grad_coef, "grad_dict": grad_dict, "scratch": scratch}, (lr, coef, dict_, grad_out))
     grad_coef = _grad_out_of(grad_coef, coef.shape, coef.dtype, want_coef, coef, "grad_coef")
     grad_dict = _grad_out_of(grad_dict, dict_.shape, torch.float32, want_dict, dict_, "grad_dict")
     d = sr_dims(n, c, h, w, scale, k, D)
@@ -502,6 +519,7 @@ def sr_dict_regress_selected_grad(lr, coef_or_sel, idx, gamma, dict_, grad_out, 
         raise ValueError("shapes of lr / coef_or_sel / idx / gamma / dict / grad_out do not agree")
     _same_device(lr, coef_or_sel=coef_or_sel, idx=idx, gamma=gamma, dict=dict_, grad_out=grad_out, grad_coef=grad_coef, grad_dict=grad_dict,
                  grad_gamma=grad_gamma, scratch=scratch)
+    _apart({"grad_coef": grad_coef, "grad_dict": grad_dict, "grad_gamma": grad_gamma, "scratch": scratch}, (lr, coef_or_sel, idx, gamma, dict_, grad_out))
     grad_coef = _grad_out_of(grad_coef, coef_or_sel.shape, coef_or_sel.dtype, want_coef, lr, "grad_coef")
     grad_dict = _grad_out_of(grad_dict, dict_.shape, torch.float32, want_dict, lr, "grad_dict")
     grad_gamma = _grad_out_of(grad_gamma, (s,), torch.float32, want_dict and gamma is not None, lr, "grad_gamma")
@@ -527,6 +545,7 @@ def sr_select_balance(coef, idx, mask=None, flags: int = 0, scratch=None):
     if idx.shape != (n, s, H, W) or (mask is not None and _dev(mask, torch.uint8, "mask").shape != (n, H, W)):
         raise ValueError("shapes of coef / idx / mask do not agree")
     _same_device(coef, idx=idx, mask=mask, scratch=scratch)
+    _apart({"scratch": scratch}, (coef, idx, mask))
     d = sr_dims(n, 1, H, W, 1, 1, D)
     lib = _lib or load_library()
     scratch = _scratch(lib.sr_select_balance_scratch_bytes(ctypes.byref(d)), scratch, coef, "sr_select_balance_scratch_bytes")
@@ -552,6 +571,7 @@ def sr_select_balance_grad(coef, slope, mask=None, weight: float = 1.0, grad_los
     if grad_coef is None and (flags & SR_GRAD_ADD):
         raise ValueError("SR_GRAD_ADD needs grad_coef")
     _same_device(coef, slope=slope, mask=mask, grad_loss=grad_loss, grad_coef=grad_coef)
+    _apart({"grad_coef": grad_coef}, (coef, slope, mask, grad_loss))
     grad_coef = _grad_out_of(grad_coef, coef.shape, coef.dtype, True, coef, "grad_coef")
     d = sr_dims(n, 1, H, W, 1, 1, D)
     status = (_lib or load_library()).sr_select_balance_grad(coef.data_ptr(), code, _ptr(mask), slope.data_ptr(), _ptr(grad_loss), weight,
@@ -593,6 +613,22 @@ class AdamwPlan:
         self._columns[:, 6] = self._sizes
         self._at = [p.data_ptr() for p in self.params]
         self._columns[:, 0] = self._at
+        self._check_apart()
+
+    def _check_apart(self):
+        """No parameter or state shares memory with another: two blocks of the step would write it."""
+        n = numpy.array(self._sizes, dtype=numpy.uint64)
+        state = 1 if self.state_bits == 8 else 4
+        columns = [(0, n * numpy.uint64(self.params[0].element_size())), (2, n * numpy.uint64(state)), (3, n * numpy.uint64(state))]
+        if self.state_bits == 8:
+            blocks = (n + numpy.uint64(ADAMW_BLOCK - 1)) // numpy.uint64(ADAMW_BLOCK) * numpy.uint64(4)
+            columns += [(4, blocks), (5, blocks)]
+        start = numpy.concatenate([self._columns[:, c] for c, _ in columns])
+        size = numpy.concatenate([b for _, b in columns])
+        start, size = start[size > 0], size[size > 0]
+        order = numpy.argsort(start)
+        if (start[order][1:] < (start + size)[order][:-1]).any():
+            raise ValueError("a parameter or state shares memory with another one of the plan")
 
     def _check(self, i):
         state = torch.float8_e4m3fn if self.state_bits == 8 else torch.float32
@@ -623,8 +659,9 @@ class AdamwPlan:
             for i, (a, b) in enumerate(zip(at, self._at)):
                 if a != b:
                     self._check(i)
-            self._at = at
             self._columns[:, 0] = at
+            self._check_apart()
+            self._at = at
 
 
 def sr_adamw_plan(params, exp_avg, exp_avg_sq, avg_scale=None, avg_sq_scale=None) -> AdamwPlan:
