@@ -293,8 +293,8 @@ grad_dict_kernel(const __grid_constant__ DictGradParams p, const CoefT* __restri
                 sPhi[q * PITCH + px] = X < W && Y < H ? load_coef(coef, plane * HW + (int64_t)Y * W + X) : 0.f;
             }
         }
-        // ---- G (threads 0 .. NPX - 1, a pixel each)
-        const int px = tid % NPX, half = tid / NPX;              // two threads a pixel, every other patch row each
+        // ---- G: two threads a pixel, every other patch row each
+        const int px = tid % NPX, half = tid / NPX;
         const int gx = X0 + px % TX, gy = Y0 + px / TX;
         const bool valid = gx < W && gy < H;
         ut.taps(pb, X0, Y0, tid, 256);

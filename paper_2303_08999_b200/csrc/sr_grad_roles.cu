@@ -316,58 +316,60 @@ template <Form FORM> __device__ __forceinline__ void load_role(const CUtensorMap
         cp_async_wait_all_();
         return;
     }
-    const int s = pb.s;
-    const bool lists = p.b.mode == kModeIdx || p.b.mode == kModeCompact;
-    const bool gather = p.b.mode == kModeGlobal && !(pb.flags & SR_COEF_COMPACT);      // (odd widths)
-    const __half zero = __ushort_as_half(0);
-    bool ok = true;
-    Tiles tl(p.b.g);
-    for (int row = pair; tl.more(p.b.g); row += p.pairs) {
-        while (tl.more(p.b.g) && row >= tl.rows) { row -= tl.rows; tl.next(p.b.g); }
-        if (!tl.more(p.b.g)) break;
-        const int item = tl.base + row, st = item % p.p_stages;
-        uint8_t* stage = sPhi + st * p.b.stage_bytes;
-        ok = wait_all(&ctl.p_empty[st], ((item / p.p_stages) & 1) ^ 1, wc, ok);
-        if (lists) {
-            if (ok)
-                for (int i = tid; i < p.b.stage_bytes / 16; i += kLoadThreads) reinterpret_cast<uint4*>(stage)[i] = make_uint4(0, 0, 0, 0);
-            ok = load_barrier_and(pair, ok);                         // (a pair leaves together: its warps meet here)
-        }
-        if (!ok) return;
-        for (int x = tid; x < 128; x += kLoadThreads) {
-            const bool inside = tl.x0 + x < pb.W;
-            uint8_t* chunk = stage + (x >> 6) * p.b.chunk_bytes;
-            const int unit = (x & 63) >> 3, at2 = (x & 7) * 2;       // this pixel's 16-byte unit and place in it
-            auto place = [&](int l) { return reinterpret_cast<__half*>(chunk + l * 128 + ((unit ^ (l & 7)) << 4) + at2); };
-            const int64_t pix = (int64_t)(tl.y0 + row) * pb.W + tl.x0 + x;
-            const __half* src = p.b.coef + (int64_t)tl.f * p.planes_in * HW + pix;
+    if constexpr (FORM == kPairs) {                          // (whatever else asks for sums has returned: plan_best)
+        const int s = pb.s;
+        const bool lists = p.b.mode == kModeIdx || p.b.mode == kModeCompact;
+        const bool gather = p.b.mode == kModeGlobal && !(pb.flags & SR_COEF_COMPACT);      // (odd widths)
+        const __half zero = __ushort_as_half(0);
+        bool ok = true;
+        Tiles tl(p.b.g);
+        for (int row = pair; tl.more(p.b.g); row += p.pairs) {
+            while (tl.more(p.b.g) && row >= tl.rows) { row -= tl.rows; tl.next(p.b.g); }
+            if (!tl.more(p.b.g)) break;
+            const int item = tl.base + row, st = item % p.p_stages;
+            uint8_t* stage = sPhi + st * p.b.stage_bytes;
+            ok = wait_all(&ctl.p_empty[st], ((item / p.p_stages) & 1) ^ 1, wc, ok);
             if (lists) {
-                const uint8_t* list = p.b.idx + (int64_t)tl.f * s * HW + pix;
-                for (int q0 = 0; inside && q0 < s; q0 += 8) {
-                    int a[8];
-                    __half v[8];
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) a[i] = q0 + i < s ? min((int)__ldg(list + (int64_t)(q0 + i) * HW), pb.D - 1) : 0;
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) v[i] = q0 + i < s ? __ldg(src + (int64_t)(p.b.mode == kModeCompact ? q0 + i : a[i]) * HW) : zero;
-#pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        if (q0 + i < s) *place(a[i]) = v[i];
-                }
-            } else {
-                for (int l0 = 0; l0 < p.b.rows; l0 += 16) {
-                    __half h[16];
-#pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        h[i] = inside && l0 + i < p.b.rows ? __ldg(src + (int64_t)(gather ? ctl.c.atoms[l0 + i] : l0 + i) * HW) : zero;
-#pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        if (l0 + i < p.b.rows) *place(l0 + i) = h[i];
+                if (ok)
+                    for (int i = tid; i < p.b.stage_bytes / 16; i += kLoadThreads) reinterpret_cast<uint4*>(stage)[i] = make_uint4(0, 0, 0, 0);
+                ok = load_barrier_and(pair, ok);                         // (a pair leaves together: its warps meet here)
+            }
+            if (!ok) return;
+            for (int x = tid; x < 128; x += kLoadThreads) {
+                const bool inside = tl.x0 + x < pb.W;
+                uint8_t* chunk = stage + (x >> 6) * p.b.chunk_bytes;
+                const int unit = (x & 63) >> 3, at2 = (x & 7) * 2;       // this pixel's 16-byte unit and place in it
+                auto place = [&](int l) { return reinterpret_cast<__half*>(chunk + l * 128 + ((unit ^ (l & 7)) << 4) + at2); };
+                const int64_t pix = (int64_t)(tl.y0 + row) * pb.W + tl.x0 + x;
+                const __half* src = p.b.coef + (int64_t)tl.f * p.planes_in * HW + pix;
+                if (lists) {
+                    const uint8_t* list = p.b.idx + (int64_t)tl.f * s * HW + pix;
+                    for (int q0 = 0; inside && q0 < s; q0 += 8) {
+                        int a[8];
+                        __half v[8];
+    #pragma unroll
+                        for (int i = 0; i < 8; ++i) a[i] = q0 + i < s ? min((int)__ldg(list + (int64_t)(q0 + i) * HW), pb.D - 1) : 0;
+    #pragma unroll
+                        for (int i = 0; i < 8; ++i) v[i] = q0 + i < s ? __ldg(src + (int64_t)(p.b.mode == kModeCompact ? q0 + i : a[i]) * HW) : zero;
+    #pragma unroll
+                        for (int i = 0; i < 8; ++i)
+                            if (q0 + i < s) *place(a[i]) = v[i];
+                    }
+                } else {
+                    for (int l0 = 0; l0 < p.b.rows; l0 += 16) {
+                        __half h[16];
+    #pragma unroll
+                        for (int i = 0; i < 16; ++i)
+                            h[i] = inside && l0 + i < p.b.rows ? __ldg(src + (int64_t)(gather ? ctl.c.atoms[l0 + i] : l0 + i) * HW) : zero;
+    #pragma unroll
+                        for (int i = 0; i < 16; ++i)
+                            if (l0 + i < p.b.rows) *place(l0 + i) = h[i];
+                    }
                 }
             }
+            fence_proxy_async_smem();
+            mbar_arrive(&ctl.p_full[st]);
         }
-        fence_proxy_async_smem();
-        mbar_arrive(&ctl.p_full[st]);
     }
 }
 
