@@ -603,17 +603,27 @@ class AdamwPlan:
         self.device, self.param_dtype = self.params[0].device, self.params[0].dtype
         self._table = (sr_adamw_tensor * count)()
         self._columns = numpy.frombuffer(self._table, dtype=numpy.uint64).reshape(count, 7)      # param, grad, m, v, m_scale, v_scale, n
-        self._states = [[t.detach() for t in tensors] for tensors in (self.m, self.v, self.m_scale, self.v_scale)]     # own references to the memory
-        for i in range(count):
-            self._check(i)
-        for column, tensors in zip((2, 3, 4, 5), self._states):
-            if tensors:
-                self._columns[:, column] = [t.data_ptr() for t in tensors]
-        self._sizes = [p.numel() for p in self.params]
+        self._states = [list(map(torch.Tensor.untyped_storage, tensors)) for tensors in (self.m, self.v, self.m_scale, self.v_scale)]    # own references to the memory
+        # (whole lists at a time: tensor by tensor the checks took as long as several steps)
+        tensor = torch.Tensor
+        self._sizes = list(map(tensor.numel, self.params))
+        parts = [(0, self.params, self.param_dtype, self._sizes), (2, self.m, self._state_dtype(), self._sizes), (3, self.v, self._state_dtype(), self._sizes)]
+        if eight:
+            blocks = [(n + ADAMW_BLOCK - 1) // ADAMW_BLOCK for n in self._sizes]
+            parts += [(4, self.m_scale, torch.float32, blocks), (5, self.v_scale, torch.float32, blocks)]
+        for column, tensors, dtype, sizes in parts:
+            if self.device.type != "cuda" or {t.dtype for t in tensors} != {dtype} or set(map(tensor.get_device, tensors)) != {self.device.index} or \
+                    not all(map(tensor.is_contiguous, tensors)) or list(map(tensor.numel, tensors)) != sizes:
+                for i in range(count):                       # which one, and what is wrong with it
+                    self._check(i)
+                raise ValueError("the tensors of a plan do not agree")
+            self._columns[:, column] = list(map(tensor.data_ptr, tensors))
         self._columns[:, 6] = self._sizes
-        self._at = [p.data_ptr() for p in self.params]
-        self._columns[:, 0] = self._at
+        self._at = list(map(tensor.data_ptr, self.params))
         self._check_apart()
+
+    def _state_dtype(self):
+        return torch.float8_e4m3fn if self.state_bits == 8 else torch.float32
 
     def _check_apart(self):
         """No parameter or state shares memory with another: two blocks of the step would write it."""
@@ -631,7 +641,7 @@ class AdamwPlan:
             raise ValueError("a parameter or state shares memory with another one of the plan")
 
     def _check(self, i):
-        state = torch.float8_e4m3fn if self.state_bits == 8 else torch.float32
+        state = self._state_dtype()
         n = self.params[i].numel()
         blocks = (n + ADAMW_BLOCK - 1) // ADAMW_BLOCK
         _dev(self.params[i], self.param_dtype, f"params[{i}]")

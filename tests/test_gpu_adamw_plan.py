@@ -42,3 +42,34 @@ def test_new_memory_at_the_old_address_is_checked():
     p.data = torch.zeros(1 << 19, device="cuda")
     with pytest.raises(ValueError):
         sr.sr_adamw_step(plan, [torch.ones(1 << 20, device="cuda")], 1, 1e-3)
+
+
+def test_a_plan_refuses_any_one_tensor_that_does_not_fit():
+    """A list is checked as a whole: whichever place the wrong tensor is at, and whichever list, it is found."""
+    def lists(bits):
+        n = [300] * 5
+        state = (lambda: [torch.zeros(x, device="cuda") for x in n]) if bits == 32 else (lambda: [torch.zeros(x, dtype=torch.float8_e4m3fn, device="cuda") for x in n])
+        out = [[torch.zeros(x, device="cuda") for x in n], state(), state()]
+        return out if bits == 32 else out + [[torch.zeros(2, device="cuda") for _ in n] for _ in range(2)]
+    for bits in (32, 8):
+        sr.sr_adamw_plan(*lists(bits))
+        for which in range(3 if bits == 32 else 5):
+            for place in (0, 2, 4):
+                for change, error in ((lambda t: t.cpu(), TypeError), (lambda t: t.to(torch.float64), TypeError), (lambda t: torch.cat([t, t])[::2], TypeError),
+                                      (lambda t: torch.cat([t, t]), ValueError), (lambda t: t[:-1], ValueError)):
+                    given = lists(bits)
+                    given[which][place] = change(given[which][place].float()).to(given[which][place].dtype) if error is ValueError else change(given[which][place])
+                    with pytest.raises(error):
+                        sr.sr_adamw_plan(*given)
+
+
+def test_a_plan_keeps_the_memory_of_its_states():
+    p, m, v = torch.zeros(1 << 18, device="cuda"), torch.zeros(1 << 18, device="cuda"), torch.zeros(1 << 18, device="cuda")
+    plan = sr.sr_adamw_plan([p], [m], [v])
+    addresses = {m.data_ptr(), v.data_ptr()}
+    m.data, v.data = torch.zeros(1, device="cuda"), torch.zeros(1, device="cuda")
+    del m, v
+    others = [torch.full((1 << 18,), 7.0, device="cuda") for _ in range(8)]            # what the allocator would put there
+    assert not addresses & {t.data_ptr() for t in others}
+    sr.sr_adamw_step(plan, [torch.ones_like(p)], 1, 1e-3)
+    assert all(bool((t == 7).all()) for t in others) and bool((p < 0).all())
