@@ -688,12 +688,15 @@ def sr_adamw_step(plan: AdamwPlan, grads, step, lr, beta1: float = 0.9, beta2: f
     _same_device(plan.params[0])
     if len(grads) != len(plan.params):
         raise ValueError("one gradient per parameter")
-    dtype, table = grads[0].dtype, plan._table
+    try:
+        dtype, dtypes, table = grads[0].dtype, {g.dtype for g in grads}, plan._table
+    except AttributeError:
+        raise TypeError("every parameter of a plan needs a gradient: leave those without one out of it") from None
     if dtype not in _ADAMW_CODES:
         raise TypeError("gradients must be float32, float16 or bfloat16")
     # (whole lists at a time: with many small tensors the step is as long as these lines)
     tensor = torch.Tensor
-    if {g.dtype for g in grads} != {dtype} or set(map(tensor.get_device, grads)) != {plan.device.index} or \
+    if dtypes != {dtype} or set(map(tensor.get_device, grads)) != {plan.device.index} or \
             not all(map(tensor.is_contiguous, grads)) or list(map(tensor.numel, grads)) != plan._sizes:
         raise TypeError(f"grads must be contiguous {dtype} tensors on {plan.device}, of their parameters' sizes")
     plan._columns[:, 1] = list(map(tensor.data_ptr, grads))

@@ -73,3 +73,14 @@ def test_a_plan_keeps_the_memory_of_its_states():
     assert not addresses & {t.data_ptr() for t in others}
     sr.sr_adamw_step(plan, [torch.ones_like(p)], 1, 1e-3)
     assert all(bool((t == 7).all()) for t in others) and bool((p < 0).all())
+
+
+@pytest.mark.parametrize("place", [0, 1])
+def test_a_parameter_without_a_gradient_is_refused_by_name(place):
+    p = [torch.zeros(10, device="cuda"), torch.zeros(20, device="cuda")]
+    plan = sr.sr_adamw_plan(p, [torch.zeros_like(x) for x in p], [torch.zeros_like(x) for x in p])
+    g = [torch.ones_like(x) for x in p]
+    g[place] = None
+    with pytest.raises(TypeError, match="needs a gradient"):
+        sr.sr_adamw_step(plan, g, 1, 1e-3)
+    assert not p[0].any() and not p[1].any()
