@@ -335,9 +335,14 @@ int sr_producer_regress(const float* lr, const void* feat, const void* folded, s
  * SR_IDX_GLOBAL, SR_COEF_COMPACT.  SR_CLAMP01 is not a flag here: zero grad_out where the forward pass clamped.
  * Distinct indices per pixel, and indices >= D, as in sr_dict_regress_selected (a repeated index of a pixel gives an unspecified
  * gradient for it; with SR_IDX_GLOBAL repeated atoms are summed).  The outputs must not overlap each other or an input.
- * Sums are held in fp32 or more; the same inputs give the same bits on every run.  A value of grad_out or of the image
- * that is not finite makes grad_coef of the pixels whose G reads it and any row of grad_dict not finite (Inf or NaN is unspecified), a
- * coefficient that is used its atom's row of grad_dict; grad_coef of other pixels is as without it.  Gradients in binary16 are rounded once: scale a small loss up (loss scaling) first.
+ * Sums are held in fp32 or more; the same inputs give the same bits on every run.  With fp32 coefficients, k = 1 or 9 or c > 4 the
+ * factors are fp32 too.  Otherwise, on the tensor cores, G and the atoms enter the products as two binary16 numbers each, 22 bits:
+ * G is right to 2^-22 of itself and 2^-35 of the tile's (8 rows of 128 pixels) largest |grad_out| times its largest |lr|, a tap to
+ * 2^-22 of itself and 2^-34 of its atom's largest, and additions to a sum of grad_dict in tensor memory are cut off (together below
+ * 1e-6 of its terms' magnitudes at 1080p).  Gradients in binary16 are rounded once: scale a small loss up (loss scaling) first.
+ * A value of grad_out or of the image that is not finite makes grad_coef of the pixels whose G reads it and any row of grad_dict
+ * not finite (Inf or NaN is unspecified), a coefficient that is used its atom's row of grad_dict; grad_coef of other pixels is
+ * as without it.
  * `scratch`: device memory of sr_dict_regress_grad_scratch_bytes(d) bytes (for the current device), 16-byte aligned, needed
  * when grad_dict or grad_gamma is asked for; the call overwrites it, and two calls that share it must not overlap.
  */

@@ -739,9 +739,11 @@ int copy_of(const Problem& pb, const void* at)
 }
 
 // Whole planes that lanes load pixel by pixel (odd widths): from how many on three pairs of load warps beat the two kernels of
-// sr_grad_tc.cu, whose every warp loads. Both gradients, 1077 x 1080, k = 5, two kernels / pairs: D = 32: 224 / 249 us, 40: 269 / 269,
-// 56: 325 / 286, 72: 538 / 310. (One pair: D = 72: 686.) Compact values and lists, 1080p x4, D = 72, s = 8, one pair / three: compact
-// 423 / 310, its dictionary sums alone 202 (two kernels' form) / 181; at k = 7 507 / 355, 699 / 265.
+// sr_grad_tc.cu, whose every warp loads. Both gradients, 1080 rows of 1077 pixels, scale 3, us, two kernels / pairs, k = 5: D = 32
+// 278 / 316, 40 333 / 349, 56 404 / 369, 72 680 / 428. The number is k = 5's. At k = 7 the pairs win from 16 planes on (16 448 / 292, 40
+// 714 / 420, 72 988 / 491), at k = 3 the two kernels up to 72 (40 251 / 305, 72 354 / 377), on small frames up to 40 (3 x 255 x 271:
+// 40 85 / 93, 72 138 / 107). Compact values and lists, 1080p x4, D = 72, s = 8, one pair / three: compact 423 / 310, its
+// dictionary sums alone 202 (two kernels' form) / 181; at k = 7 507 / 355, 699 / 265.
 constexpr int kPairsPlanes = 40;
 bool one_by_one(const GradArgs& a) { return (a.gdict || a.ggamma) && a.mode != kModeIdx && a.mode != kModeCompact && copy_of(a.pb, a.coef) == 0; }
 
