@@ -452,11 +452,9 @@ balance_grad_kernel(const CoefT* __restrict__ coef, CoefT* __restrict__ grad, co
     get_pixels<PX, VEC>(k, sk, lane);
     get_pixels<PX, VEC>(c, sc, lane);
     bool all = true;                             // this warp's pixels all count
-    if (ADD) {
 #pragma unroll
-        for (int i = 0; i < PX; ++i) all &= k[i] != 0.f;
-        all = __all_sync(0xffffffffu, all);
-    }
+    for (int i = 0; i < PX; ++i) all &= k[i] != 0.f;
+    all = __all_sync(0xffffffffu, all);
     auto finish = [&](auto every) {              // `every`: all pixels of the warp count
 #pragma unroll
     for (int j = 0; j < AW; ++j) {
@@ -481,7 +479,7 @@ balance_grad_kernel(const CoefT* __restrict__ coef, CoefT* __restrict__ grad, co
 #pragma unroll
             for (int i = 0; i < PER; ++i) d[i] = fmaf(a, k[w * PER + i], c[w * PER + i]);
             o[w] = result_word<ADD>((const CoefT*)nullptr, x[j][w], old[w], d);
-            if (ADD && !decltype(every)::value) {                   // a pixel that does not count keeps its bits
+            if (!decltype(every)::value) {       // a pixel that does not count keeps its bits, or is zero, whatever the weight is
 #pragma unroll
                 for (int i = 0; i < PER; ++i) {
                     const uint32_t part = PER == 1 ? 0xFFFFFFFFu : 0xFFFFu << (16 * i);
@@ -502,7 +500,7 @@ balance_grad_kernel(const CoefT* __restrict__ coef, CoefT* __restrict__ grad, co
         }
     }
     };
-    if (!ADD || all) finish(std::true_type{});
+    if (all) finish(std::true_type{});
     else finish(std::false_type{});
 }
 

@@ -347,21 +347,21 @@ template <Form FORM> __device__ __forceinline__ void load_role(const CUtensorMap
                     for (int q0 = 0; inside && q0 < s; q0 += 8) {
                         int a[8];
                         __half v[8];
-    #pragma unroll
+#pragma unroll
                         for (int i = 0; i < 8; ++i) a[i] = q0 + i < s ? min((int)__ldg(list + (int64_t)(q0 + i) * HW), pb.D - 1) : 0;
-    #pragma unroll
+#pragma unroll
                         for (int i = 0; i < 8; ++i) v[i] = q0 + i < s ? __ldg(src + (int64_t)(p.b.mode == kModeCompact ? q0 + i : a[i]) * HW) : zero;
-    #pragma unroll
+#pragma unroll
                         for (int i = 0; i < 8; ++i)
                             if (q0 + i < s) *place(a[i]) = v[i];
                     }
                 } else {
                     for (int l0 = 0; l0 < p.b.rows; l0 += 16) {
                         __half h[16];
-    #pragma unroll
+#pragma unroll
                         for (int i = 0; i < 16; ++i)
                             h[i] = inside && l0 + i < p.b.rows ? __ldg(src + (int64_t)(gather ? ctl.c.atoms[l0 + i] : l0 + i) * HW) : zero;
-    #pragma unroll
+#pragma unroll
                         for (int i = 0; i < 16; ++i)
                             if (l0 + i < p.b.rows) *place(l0 + i) = h[i];
                     }

@@ -45,3 +45,25 @@ def test_sums_near_the_smallest_normal_number(size, weight, W):
     inside &= np.abs(want) < 3e38
     bound = bound + 2 * U32 * np.abs(want)
     assert np.all(np.abs(added - want)[inside] <= bound[inside])
+
+
+@pytest.mark.parametrize("bad", [np.inf, -np.inf, np.nan])
+@pytest.mark.parametrize("dt,W", [("f32", 24), ("f16", 24), ("f32", 23), ("f16", 23)])
+def test_a_weight_that_is_not_finite_stays_with_the_pixels_that_count(dt, W, bad):
+    """An overflowed loss scale: pixels that do not count (masked, or with a sum of zero) are zero, or keep their bits, all the same."""
+    rng = np.random.default_rng(5)
+    coef = rng.uniform(0.1, 1.0, (2, 24, 20, W)).astype(np.float16 if dt == "f16" else np.float32)
+    coef[1, :, 3, 2:9] = 0
+    mask = np.ones((2, 20, W), np.uint8)
+    mask[0, 5:, 7:] = 0
+    mask[1, :, ::3] = 0
+    idx = oracle.dict_select(coef, 4)
+    slope = sr.sr_select_balance(to(coef), to(idx), to(mask))[3]
+    off = np.broadcast_to(((mask == 0) | (np.abs(coef).sum(1) == 0))[:, None], coef.shape)
+    loss_grad = to(np.array([bad], np.float32))
+    start = rng.normal(0, 1, coef.shape).astype(coef.dtype)
+    for kw in ({"weight": 2.0, "grad_loss": loss_grad}, {"weight": float(bad)}):
+        grad = host(sr.sr_select_balance_grad(to(coef), slope, to(mask), **kw))
+        assert not np.any(grad[off]) and not np.isfinite(grad[~off]).any()
+        grad = host(sr.sr_select_balance_grad(to(coef), slope, to(mask), flags=sr.SR_GRAD_ADD, grad_coef=to(start.copy()), **kw))
+        assert np.array_equal(grad[off], start[off]) and not np.isfinite(grad[~off]).any()
