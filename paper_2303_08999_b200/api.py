@@ -436,20 +436,18 @@ def _same_device(first, **others):
             raise ValueError(f"{what} is on {t.device}, lr or coef on {first.device}")
 
 
-def _span(t):
-    at = t.data_ptr()
-    return at, at + t.numel() * t.element_size()
-
-
-def _apart(written: dict, read: tuple) -> None:
-    """The caller's tensors that a call writes share no memory with each other or with what it reads. (New ones never do.)"""
-    spans = [(*_span(t), what) for what, t in written.items() if t is not None]
-    if not spans:
-        return
-    others = [_span(t) for t in read if t is not None]
-    for i, (a, b, what) in enumerate(spans):
-        if any(a < d and c < b for c, d in others) or any(a < d and c < b for c, d, _ in spans[:i]):
-            raise ValueError(f"{what} shares memory with another tensor of the call")
+def _apart(written: tuple, read: tuple) -> None:
+    """The caller's tensors that a call writes, as (name, tensor), share no memory with each other or with what it reads. (New ones never do.)"""
+    for i, (what, t) in enumerate(written):
+        if t is None:
+            continue
+        first = t.data_ptr()
+        end = first + t.nbytes
+        for other in read + tuple(o for _, o in written[:i]):
+            if other is not None:
+                at = other.data_ptr()
+                if first < at + other.nbytes and at < end:
+                    raise ValueError(f"{what} shares memory with another tensor of the call")
 
 
 # The kernels write through addresses, which autograd does not see: what a caller's tensor is written for is said here, so that a backward
@@ -483,7 +481,7 @@ def sr_dict_regress_dense_grad(lr, coef, dict_, grad_out, scale: int, k: int, fl
     if dict_.shape != (D, k * k) or coef.shape != (n, D, H, W) or grad_out.shape != (n, c, H, W):
         raise ValueError("shapes of lr / coef / dict / grad_out do not agree")
     _same_device(lr, coef=coef, dict=dict_, grad_out=grad_out, grad_coef=grad_coef, grad_dict=grad_dict, scratch=scratch)
-    _apart({"grad_coef": grad_coef, "grad_dict": grad_dict, "scratch": scratch}, (lr, coef, dict_, grad_out))
+    _apart((("grad_coef", grad_coef), ("grad_dict", grad_dict), ("scratch", scratch)), (lr, coef, dict_, grad_out))
     grad_coef = _grad_out_of(grad_coef, coef.shape, coef.dtype, want_coef, coef, "grad_coef")
     grad_dict = _grad_out_of(grad_dict, dict_.shape, torch.float32, want_dict, dict_, "grad_dict")
     d = sr_dims(n, c, h, w, scale, k, D)
@@ -519,7 +517,7 @@ def sr_dict_regress_selected_grad(lr, coef_or_sel, idx, gamma, dict_, grad_out, 
         raise ValueError("shapes of lr / coef_or_sel / idx / gamma / dict / grad_out do not agree")
     _same_device(lr, coef_or_sel=coef_or_sel, idx=idx, gamma=gamma, dict=dict_, grad_out=grad_out, grad_coef=grad_coef, grad_dict=grad_dict,
                  grad_gamma=grad_gamma, scratch=scratch)
-    _apart({"grad_coef": grad_coef, "grad_dict": grad_dict, "grad_gamma": grad_gamma, "scratch": scratch}, (lr, coef_or_sel, idx, gamma, dict_, grad_out))
+    _apart((("grad_coef", grad_coef), ("grad_dict", grad_dict), ("grad_gamma", grad_gamma), ("scratch", scratch)), (lr, coef_or_sel, idx, gamma, dict_, grad_out))
     grad_coef = _grad_out_of(grad_coef, coef_or_sel.shape, coef_or_sel.dtype, want_coef, lr, "grad_coef")
     grad_dict = _grad_out_of(grad_dict, dict_.shape, torch.float32, want_dict, lr, "grad_dict")
     grad_gamma = _grad_out_of(grad_gamma, (s,), torch.float32, want_dict and gamma is not None, lr, "grad_gamma")
@@ -545,7 +543,7 @@ def sr_select_balance(coef, idx, mask=None, flags: int = 0, scratch=None):
     if idx.shape != (n, s, H, W) or (mask is not None and _dev(mask, torch.uint8, "mask").shape != (n, H, W)):
         raise ValueError("shapes of coef / idx / mask do not agree")
     _same_device(coef, idx=idx, mask=mask, scratch=scratch)
-    _apart({"scratch": scratch}, (coef, idx, mask))
+    _apart((("scratch", scratch),), (coef, idx, mask))
     d = sr_dims(n, 1, H, W, 1, 1, D)
     lib = _lib or load_library()
     scratch = _scratch(lib.sr_select_balance_scratch_bytes(ctypes.byref(d)), scratch, coef, "sr_select_balance_scratch_bytes")
@@ -571,7 +569,7 @@ def sr_select_balance_grad(coef, slope, mask=None, weight: float = 1.0, grad_los
     if grad_coef is None and (flags & SR_GRAD_ADD):
         raise ValueError("SR_GRAD_ADD needs grad_coef")
     _same_device(coef, slope=slope, mask=mask, grad_loss=grad_loss, grad_coef=grad_coef)
-    _apart({"grad_coef": grad_coef}, (coef, slope, mask, grad_loss))
+    _apart((("grad_coef", grad_coef),), (coef, slope, mask, grad_loss))
     grad_coef = _grad_out_of(grad_coef, coef.shape, coef.dtype, True, coef, "grad_coef")
     d = sr_dims(n, 1, H, W, 1, 1, D)
     status = (_lib or load_library()).sr_select_balance_grad(coef.data_ptr(), code, _ptr(mask), slope.data_ptr(), _ptr(grad_loss), weight,
